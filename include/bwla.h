@@ -56,6 +56,7 @@ enum {
 
 #define BWLA_DTYPE_F32 0
 #define BWLA_DTYPE_BF16 1
+#define BWLA_DTYPE_F16 2        /* (rows to quantise to 4 bits only) */
 
 /*
  * Binarise already rotated/centred weights: packed[n][k>>5] bit (k&31) = (W'[n][k] > 0).   (Eq. 2-3)
@@ -243,6 +244,95 @@ int bwla_layer_rotate_quant_asym(const bwla_layer* layer, const void* x_bf16, in
 size_t bwla_group_workspace_bytes(const bwla_layer* const* layers, int count, int64_t M);
 int bwla_w1ax_linear_group(const bwla_layer* const* layers, int count, const void* x_bf16, int64_t M, int64_t ldx,
                            void* const* outs, const int64_t* ldos, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Microscaled 4-bit floating point --------------------------------------------------------------------------
+ * For linears that stay out of the binarisation (first and last blocks, sensitive projections, the output head), in the
+ * same rotated coordinates: weights and activations as e2m1 values (0, .5, 1, 1.5, 2, 3, 4, 6 and signs) with a scale a
+ * block of neighbouring k.  (The paper has no counterpart; it compares against 4-bit integer methods.)
+ *
+ *   BWLA_FP4_MX  blocks of 32, scale 2^(byte - 127), byte 255 for NaN (OCP Microscaling Formats 1.0, MXFP4).  The quantiser
+ *                takes e = max(floor(log2 max|x|) - 2, -127) and code = e2m1(x 2^-e); a block of zeros has byte 0.
+ *   BWLA_FP4_NV  blocks of 16, an e4m3 scale byte, and an fp32 scale a row.  The quantiser takes the smallest power of two
+ *                2^E >= 2^-126 with max|row| <= 6 * 448 * 2^E for the row (1 for a row of zeros), the block's
+ *                max|x| / (6 2^E) to nearest e4m3, at least 2^-9, as its scale s (0 for a block of zeros), and
+ *                code = e2m1(x / (s 2^E)).
+ * Rounding is to nearest, ties to the even code, beyond 6 to 6; the quotients are exact, so codes do not depend on the shape
+ * or the kernel.  A block (MX) or a row (NV) with an infinity or a NaN in it stands for NaN throughout: scale byte 255, or
+ * a NaN row scale, with codes of zero.
+ *
+ * An operand of `rows` rows and K columns (K a positive multiple of 32, at most 2^24):
+ *   codes      uint8 [rows][K/2], 16-byte aligned: k even in the low, k odd in the high half of byte k/2
+ *   scales     bwla_fp4_scale_bytes(rows, K, format) bytes, 16-byte aligned: tiles of 128 rows x 4 blocks, 512 bytes each, the tiles
+ *              of the same 128 rows one after the other; in a tile block j of row r is byte (r % 32) * 16 + (r / 32) * 4 + j.
+ *              Blocks that fill up a row's last tile must be zero (the quantiser writes them); rows beyond the last may hold anything.
+ *   row_scales fp32 [rows], or NULL for ones
+ */
+enum { BWLA_FP4_MX = 0, BWLA_FP4_NV = 1 };
+size_t bwla_fp4_scale_bytes(int64_t rows, int64_t K, int format);      /* 0 for sizes that are not taken, or no rows */
+
+/*
+ * Rows (activations or weights) to codes and scales.
+ *   x     device, [M][ldx] of `dtype` (BWLA_DTYPE_F32, BF16 or F16), ldx >= K
+ *   row_scales is written for BWLA_FP4_NV and not used for BWLA_FP4_MX.  M == 0 is a no-op.
+ * The outputs may be weights of the next call on `stream` without a synchronisation (no call starts before this one has ended).
+ */
+int bwla_fp4_quantize_rows(const void* x, int dtype, int64_t M, int64_t K, int64_t ldx, int format,
+                           uint8_t* codes, uint8_t* scales, float* row_scales, void* stream);
+
+/*
+ * The values that codes stand for: code * block scale (exact) * row scale in fp32, rounded to `dtype` (BWLA_DTYPE_F32 or BF16).
+ * What the quantiser has made comes back exactly in either type.   out device [M][ldo], ldo >= K
+ */
+int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const float* row_scales, int64_t M, int64_t K, int format,
+                         void* out, int dtype, int64_t ldo, void* stream);
+
+/*
+ * Product of two operands of one format, M rows of activations and N rows of weights:
+ *   out[m][n] = bf16( a_rows[m] * w_rows[n] * sum_k a[m][k] * w[n][k] )
+ * with fp32 sums on the block-scaled tensor cores (their accumulation truncates: a sum over K is off by at most K/64 units
+ * of 2^-23 of its largest partial sum).
+ *   out_bf16  device, bf16 [M][ldo], ldo >= N; columns beyond N are left as they are.  M == 0 or N == 0 is a no-op.
+ *   workspace device, 256-byte aligned, of bwla_fp4_gemm_workspace_bytes; its first 256 bytes (status words) must be zero
+ *     before the first call; bwla_check_status applies to it
+ */
+size_t bwla_fp4_gemm_workspace_bytes(int64_t M, int64_t K, int64_t N);
+int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_rows, int64_t M, int64_t K,
+                        const uint8_t* w_codes, const uint8_t* w_scales, const float* w_rows, int64_t N, int format,
+                        void* out_bf16, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Online OKT (Sec. 3.1) and the quantiser above: codes and scales of Y_t = P1^T * reshape(x_t, n1 x n2) * P2, for activations and, with
+ * rows of a weight matrix as x, for the weights that meet them.  Y has the accuracy of bwla_rotate_quant_act's (1e-6 of a token's
+ * full scale); a code or block scale can differ from the exact Y's only where that decides.
+ *   x_bf16 device, bf16 [M][ldx]; P1, P2 as for bwla_rotate_quant_act.  Factor sizes the tensor-core rotation does not take
+ *   (n2 % 8 != 0, n2 > 256, n1 > 192) return BWLA_ERR_UNSUPPORTED.
+ *   workspace of bwla_rotate_quant_fp4_workspace_bytes, its first 256 bytes as above
+ */
+size_t bwla_rotate_quant_fp4_workspace_bytes(int64_t M, int64_t K);
+int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const float* P1, int n1, const float* P2, int n2,
+                          int format, uint8_t* codes, uint8_t* scales, float* row_scales, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * A prepared 4-bit layer: the factors in the form the kernels read (in `prepared`, 256-byte aligned, of
+ * bwla_fp4_layer_prepared_bytes) and the caller's quantised weights of the rotated coordinates, N rows.  As for bwla_layer, the
+ * handle owns no device memory and the caller keeps all of it alive and unchanged until bwla_fp4_layer_destroy.
+ *   bwla_fp4_layer_rotate_quant  what bwla_rotate_quant_fp4 computes
+ *   bwla_fp4_layer_linear        out[t][n] = the product of the quantised Y_t with the weights, one call; workspace of
+ *                                bwla_fp4_layer_workspace_bytes, its first 256 bytes as above
+ */
+typedef struct bwla_fp4_layer bwla_fp4_layer;
+size_t bwla_fp4_layer_prepared_bytes(int64_t K, int n1, int n2);
+int bwla_fp4_layer_create(bwla_fp4_layer** layer, int64_t K, int64_t N, const float* P1, int n1, const float* P2, int n2, int format,
+                          const uint8_t* w_codes, const uint8_t* w_scales, const float* w_rows, void* prepared,
+                          size_t prepared_bytes, void* stream);
+void bwla_fp4_layer_destroy(bwla_fp4_layer* layer);
+int bwla_fp4_layer_rotate_quant(const bwla_fp4_layer* layer, const void* x_bf16, int64_t M, int64_t ldx, uint8_t* codes,
+                                uint8_t* scales, float* row_scales, void* workspace, size_t workspace_bytes, void* stream);
+size_t bwla_fp4_layer_workspace_bytes(const bwla_fp4_layer* layer, int64_t M);
+int bwla_fp4_layer_linear(const bwla_fp4_layer* layer, const void* x_bf16, int64_t M, int64_t ldx, void* out_bf16, int64_t ldo,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Contraction + epilogue from given codes (the part of the layer after the quantiser), so that

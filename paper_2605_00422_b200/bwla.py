@@ -39,7 +39,11 @@ EXPORTS = [
     "bwla_workspace_section", "bwla_force_rotation", "bwla_layer_prepared_bytes", "bwla_layer_create",
     "bwla_layer_destroy", "bwla_layer_rotate_quant", "bwla_group_workspace_bytes", "bwla_w1ax_linear_group",
     "bwla_layer_set_activation_quant", "bwla_layer_rotate_quant_asym", "bwla_binarize_workspace_bytes",
-    "bwla_binarize_rows", "bwla_w1a16_workspace_bytes", "bwla_layer_w1a16_linear",
+    "bwla_binarize_rows", "bwla_w1a16_workspace_bytes", "bwla_layer_w1a16_linear", "bwla_fp4_scale_bytes",
+    "bwla_fp4_quantize_rows", "bwla_fp4_expand_rows", "bwla_fp4_gemm_workspace_bytes", "bwla_fp4_gemm_codes",
+    "bwla_rotate_quant_fp4_workspace_bytes", "bwla_rotate_quant_fp4", "bwla_fp4_layer_prepared_bytes",
+    "bwla_fp4_layer_create", "bwla_fp4_layer_destroy", "bwla_fp4_layer_rotate_quant", "bwla_fp4_layer_workspace_bytes",
+    "bwla_fp4_layer_linear",
 ]
 
 
@@ -89,6 +93,23 @@ def _load() -> C.CDLL:
     lib.bwla_w1a16_workspace_bytes.argtypes = [vp, i64]
     lib.bwla_w1a16_workspace_bytes.restype = sz
     lib.bwla_layer_w1a16_linear.argtypes = [vp, vp, i64, i64, vp, i64, vp, sz, vp]
+    lib.bwla_fp4_scale_bytes.argtypes = [i64, i64, ci]
+    lib.bwla_fp4_quantize_rows.argtypes = [vp, ci, i64, i64, i64, ci, vp, vp, vp, vp]
+    lib.bwla_fp4_expand_rows.argtypes = [vp, vp, vp, i64, i64, ci, vp, ci, i64, vp]
+    lib.bwla_fp4_gemm_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.bwla_fp4_gemm_codes.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp, i64, ci, vp, i64, vp, sz, vp]
+    lib.bwla_rotate_quant_fp4_workspace_bytes.argtypes = [i64, i64]
+    lib.bwla_rotate_quant_fp4.argtypes = [vp, i64, i64, i64, vp, ci, vp, ci, ci, vp, vp, vp, vp, sz, vp]
+    lib.bwla_fp4_layer_prepared_bytes.argtypes = [i64, ci, ci]
+    lib.bwla_fp4_layer_create.argtypes = [C.POINTER(vp), i64, i64, vp, ci, vp, ci, ci, vp, vp, vp, vp, sz, vp]
+    lib.bwla_fp4_layer_destroy.argtypes = [vp]
+    lib.bwla_fp4_layer_destroy.restype = None
+    lib.bwla_fp4_layer_rotate_quant.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.bwla_fp4_layer_workspace_bytes.argtypes = [vp, i64]
+    lib.bwla_fp4_layer_linear.argtypes = [vp, vp, i64, i64, vp, i64, vp, sz, vp]
+    for name in ("bwla_fp4_scale_bytes", "bwla_fp4_gemm_workspace_bytes", "bwla_rotate_quant_fp4_workspace_bytes",
+                 "bwla_fp4_layer_prepared_bytes", "bwla_fp4_layer_workspace_bytes"):
+        getattr(lib, name).restype = sz
     lib.bwla_group_workspace_bytes.argtypes = [C.POINTER(vp), ci, i64]
     lib.bwla_group_workspace_bytes.restype = sz
     lib.bwla_w1ax_linear_group.argtypes = [C.POINTER(vp), ci, vp, i64, i64, C.POINTER(vp), C.POINTER(i64), vp, sz, vp]
@@ -120,6 +141,8 @@ def _load_calls():
     loader.exec_module(mod)
     mod.bind(*(C.cast(f, C.c_void_p).value for f in (_lib.bwla_w1ax_linear_group, _lib.bwla_w1ax_linear, _lib.bwla_layer_w1a16_linear,
                                                      _lib.bwla_pack_signs)))
+    mod.bind_fp4(*(C.cast(f, C.c_void_p).value for f in (_lib.bwla_fp4_quantize_rows, _lib.bwla_fp4_expand_rows, _lib.bwla_fp4_gemm_codes,
+                                                         _lib.bwla_fp4_layer_linear)))
     return mod
 
 
@@ -396,6 +419,177 @@ def bwla_layer_rotate_quant(layer: Layer, x: torch.Tensor, want_y: bool = False)
                                       _ptr(y), _stream())
     _check(st, "bwla_layer_rotate_quant")
     return codes, scales, y
+
+
+# ---- microscaled 4-bit floating point ----------------------------------------------------------------------------
+BWLA_FP4_MX, BWLA_FP4_NV = 0, 1
+
+
+def bwla_fp4_scale_bytes(rows: int, K: int, format: int) -> int:
+    return int(_lib.bwla_fp4_scale_bytes(rows, K, format))
+
+
+def _fp4_outputs(rows: int, K: int, format: int, device):
+    """(codes uint8 [rows][K/2], scale tiles uint8, row scales fp32 [rows] or None) to be written by a quantiser."""
+    codes = torch.empty((rows, K // 2), dtype=torch.uint8, device=device)
+    scales = torch.empty(bwla_fp4_scale_bytes(rows, K, format), dtype=torch.uint8, device=device)
+    return codes, scales, torch.empty(rows, dtype=torch.float32, device=device) if format == BWLA_FP4_NV else None
+
+
+def bwla_fp4_quantize_rows(x: torch.Tensor, format: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                           row_scales: Optional[torch.Tensor] = None):
+    """x: fp32, bf16 or fp16 [M][K] (row stride >= K) -> (codes uint8 [M][K/2], scale tiles uint8, row scales fp32 [M] or None)."""
+    if codes is None or scales is None or (row_scales is None and format == BWLA_FP4_NV):
+        made = _fp4_outputs(x.shape[0], x.shape[-1], format, x.device)
+        codes, scales = made[0] if codes is None else codes, made[1] if scales is None else scales
+        row_scales = made[2] if row_scales is None else row_scales
+    st = _calls.fp4_quantize(x, format, codes, scales, row_scales)
+    if st:
+        _check(st, "bwla_fp4_quantize_rows")
+    return codes, scales, row_scales
+
+
+def bwla_fp4_expand_rows(codes: torch.Tensor, scales: torch.Tensor, row_scales: Optional[torch.Tensor], format: int,
+                         out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
+    """The values [M][K] (bf16, or fp32) that quantised rows stand for."""
+    if out is None:
+        out = torch.empty((codes.shape[0], 2 * codes.shape[-1]), dtype=dtype, device=codes.device)
+    st = _calls.fp4_expand(codes, scales, row_scales, format, out)
+    if st:
+        _check(st, "bwla_fp4_expand_rows")
+    return out
+
+
+def bwla_fp4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
+    return int(_lib.bwla_fp4_gemm_workspace_bytes(M, K, N))
+
+
+def new_fp4_workspace(M: int, K: int, N: int, device="cuda") -> torch.Tensor:
+    """Scratch buffer for bwla_fp4_gemm_codes (zero-filled)."""
+    n = bwla_fp4_gemm_workspace_bytes(M, K, N)
+    if n == 0:
+        raise ValueError("invalid dimensions")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def bwla_fp4_gemm_codes(a_codes: torch.Tensor, a_scales: torch.Tensor, a_rows: Optional[torch.Tensor], w_codes: torch.Tensor,
+                        w_scales: torch.Tensor, w_rows: Optional[torch.Tensor], format: int, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Product of quantised rows [M][K] and [N][K] (codes, scale tiles, row scales or None each): bf16 out [M][N]."""
+    if out is None:
+        out = torch.empty((a_codes.shape[0], w_codes.shape[0]), dtype=torch.bfloat16, device=a_codes.device)
+    if workspace is None:
+        workspace = new_fp4_workspace(a_codes.shape[0], 2 * a_codes.shape[-1], w_codes.shape[0], a_codes.device)
+    st = _calls.fp4_gemm(a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, format, out, workspace)
+    if st:
+        _check(st, "bwla_fp4_gemm_codes")
+    return out
+
+
+def bwla_rotate_quant_fp4_workspace_bytes(M: int, K: int) -> int:
+    return int(_lib.bwla_rotate_quant_fp4_workspace_bytes(M, K))
+
+
+def bwla_rotate_quant_fp4(x: torch.Tensor, P1: torch.Tensor, P2: torch.Tensor, format: int, workspace: Optional[torch.Tensor] = None):
+    """x: bf16 [M][K] -> (codes, scale tiles, row scales or None) of the rows rotated by P1 (x) P2."""
+    _need(x, torch.bfloat16, "x", 2)
+    _need(P1, torch.float32, "P1", 2)
+    _need(P2, torch.float32, "P2", 2)
+    if not (P1.is_contiguous() and P2.is_contiguous()):
+        raise TypeError("P1 and P2 must be contiguous")
+    M, K = x.shape
+    if workspace is None:
+        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, K)), dtype=torch.uint8, device=x.device)
+    codes, scales, rows = _fp4_outputs(M, K, format, x.device)
+    st = _lib.bwla_rotate_quant_fp4(_ptr(x), M, K, x.stride(0) if M > 0 else K, _ptr(P1), P1.shape[0], _ptr(P2), P2.shape[0], format, _ptr(codes),
+                                    _ptr(scales), _ptr(rows), _ptr(workspace), workspace.numel(), _stream())
+    _check(st, "bwla_rotate_quant_fp4")
+    return codes, scales, rows
+
+
+class Fp4Layer:
+    """A prepared 4-bit layer (bwla_fp4_layer_create): keeps the handle, the tensors it points into and the prepared buffer."""
+
+    def __init__(self, P1, P2, format, w_codes, w_scales, w_rows=None):
+        _need(P1, torch.float32, "P1", 2)
+        _need(P2, torch.float32, "P2", 2)
+        _need(w_codes, torch.uint8, "w_codes", 2)
+        _need(w_scales, torch.uint8, "w_scales", 1)
+        if w_rows is not None:
+            _need(w_rows, torch.float32, "w_rows", 1)
+        if not (w_codes.is_contiguous() and P1.is_contiguous() and P2.is_contiguous()):
+            raise TypeError("w_codes, P1 and P2 must be contiguous")
+        self.N, self.K, self.format = w_codes.shape[0], 2 * w_codes.shape[1], format
+        self.n1, self.n2 = P1.shape[0], P2.shape[0]
+        if w_scales.numel() < bwla_fp4_scale_bytes(self.N, self.K, format) or (w_rows is not None and w_rows.numel() != self.N):
+            raise TypeError("w_scales or w_rows: too small for the rows of w_codes")
+        self.tensors = (P1, P2, w_codes, w_scales, w_rows)
+        self.handle = C.c_void_p()
+        nbytes = int(_lib.bwla_fp4_layer_prepared_bytes(self.K, self.n1, self.n2))
+        if nbytes == 0:
+            raise BwlaError(BWLA_ERR_INVALID_ARG, "bwla_fp4_layer_prepared_bytes")
+        self.prepared = torch.empty(nbytes, dtype=torch.uint8, device=w_codes.device)
+        st = _lib.bwla_fp4_layer_create(C.byref(self.handle), self.K, self.N, _ptr(P1), self.n1, _ptr(P2), self.n2, format, _ptr(w_codes),
+                                        _ptr(w_scales), _ptr(w_rows), _ptr(self.prepared), nbytes, _stream())
+        _check(st, "bwla_fp4_layer_create")
+        self._fp4 = self.handle.value                # (what the native calls read; of another name than a Layer's, which they must not take)
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h is not None and h.value and _lib is not None:
+            _lib.bwla_fp4_layer_destroy(h)
+            self.handle = C.c_void_p()
+            self._fp4 = 0
+
+
+def bwla_fp4_layer_prepared_bytes(K: int, n1: int, n2: int) -> int:
+    return int(_lib.bwla_fp4_layer_prepared_bytes(K, n1, n2))
+
+
+def bwla_fp4_layer_create(P1, P2, format, w_codes, w_scales, w_rows=None) -> Fp4Layer:
+    """Prepares a 4-bit layer's factors once (launches on the current stream) and returns the handle object."""
+    return Fp4Layer(P1, P2, format, w_codes, w_scales, w_rows)
+
+
+def bwla_fp4_layer_destroy(layer: Fp4Layer) -> None:
+    layer.__del__()
+
+
+def bwla_fp4_layer_rotate_quant(layer: Fp4Layer, x: torch.Tensor, workspace: Optional[torch.Tensor] = None):
+    """x: bf16 [M][K] -> (codes, scale tiles, row scales or None) of the rotated rows, through a prepared layer."""
+    _need(x, torch.bfloat16, "x", 2)
+    M = x.shape[0]
+    if x.shape[1] != layer.K:
+        raise TypeError("x must be [M][K] of the layer")
+    if workspace is None:
+        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, layer.K)), dtype=torch.uint8, device=x.device)
+    codes, scales, rows = _fp4_outputs(M, layer.K, layer.format, x.device)
+    st = _lib.bwla_fp4_layer_rotate_quant(layer.handle, _ptr(x), M, x.stride(0) if M > 0 else layer.K, _ptr(codes), _ptr(scales), _ptr(rows),
+                                          _ptr(workspace), workspace.numel(), _stream())
+    _check(st, "bwla_fp4_layer_rotate_quant")
+    return codes, scales, rows
+
+
+def bwla_fp4_layer_workspace_bytes(layer: Fp4Layer, M: int) -> int:
+    return int(_lib.bwla_fp4_layer_workspace_bytes(layer.handle, M))
+
+
+def new_fp4_layer_workspace(layer: Fp4Layer, M: int, device="cuda") -> torch.Tensor:
+    """Scratch buffer for bwla_fp4_layer_linear (zero-filled)."""
+    return torch.zeros(max(256, bwla_fp4_layer_workspace_bytes(layer, M)), dtype=torch.uint8, device=device)
+
+
+def bwla_fp4_layer_linear(layer: Fp4Layer, x: torch.Tensor, out: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The prepared 4-bit layer: bf16 x [M][K] -> bf16 out [M][N]."""
+    if out is None:
+        out = torch.empty((x.shape[0], layer.N), dtype=torch.bfloat16, device=x.device)
+    if workspace is None:
+        workspace = new_fp4_layer_workspace(layer, x.shape[0], x.device)
+    st = _calls.fp4_linear(layer, x, out, workspace)
+    if st:
+        _check(st, "bwla_fp4_layer_linear")
+    return out
 
 
 def _handles(layers):

@@ -41,7 +41,7 @@ void prof_end(int kind, cudaStream_t stream) {
 static bool valid_bits(int bits) { return bits == 4 || bits == 6 || bits == 8; }
 
 // The compute entry points need an sm_100 device to be current.
-static int check_device() {
+int check_device() {
     int dev = 0, major = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) { g_last_cuda_error = (int)e; cudaGetLastError(); return BWLA_ERR_UNSUPPORTED; }
@@ -50,7 +50,7 @@ static int check_device() {
     return major == 10 ? BWLA_OK : BWLA_ERR_UNSUPPORTED;
 }
 
-static bool valid_rotation_dims(int64_t K, int n1, int n2) {
+bool valid_rotation_dims(int64_t K, int n1, int n2) {
     return K > 0 && K % 32 == 0 && K <= 25600 && n1 > 0 && n2 > 0 && (int64_t)n1 * n2 == K;
 }
 
@@ -311,6 +311,22 @@ static PreparedLayout prepared_layout(int n1, int n2) {
     return p;
 }
 
+}  // extern "C"
+
+size_t bwla::prepared_factor_bytes(int n1, int n2) { return prepared_layout(n1, n2).rowsum; }
+int bwla::prepare_factors(int n1, int n2, const float* P1, const float* P2, uint8_t* prepared, PreparedFactors* out, cudaStream_t stream) {
+    const PreparedLayout lay = prepared_layout(n1, n2);
+    out->geom = lay.geom;
+    out->base = prepared;
+    out->many = lay.has_rows || lay.has_okt ? prepared + lay.many : nullptr;
+    int st = launch_prepare_rot(lay.geom, P1, P2, prepared, stream);
+    if (st == BWLA_OK && lay.has_rows) st = launch_prepare_rows(lay.rows_geom, P1, P2, out->many, stream);
+    if (st == BWLA_OK && lay.has_okt) st = launch_prepare_okt(lay.okt_geom, P1, P2, out->many, stream);
+    return st;
+}
+
+extern "C" {
+
 size_t bwla_layer_prepared_bytes(int64_t K, int64_t N, int n1, int n2, int r) {
     if (!valid_rotation_dims(K, n1, n2) || N < 0 || r < 0 || r > 256) return 0;
     // the terms of the Kronecker factors for the tensor-core rotations, then the sign sums of the rows
@@ -336,15 +352,14 @@ int bwla_layer_create(bwla_layer** layer, int64_t K, int64_t N, const float* P1,
     L->P1 = P1; L->P2 = P2; L->packed = packed; L->alpha = alpha; L->mu = mu; L->U = U_bf16; L->V = V_bf16;
     L->prepared = (uint8_t*)prepared;
     const PreparedLayout lay = prepared_layout(n1, n2);
-    L->rot = lay.rot; L->geom = lay.geom;
-    L->many = lay.has_rows || lay.has_okt ? L->prepared + lay.many : nullptr;
+    L->rot = lay.rot; L->geom = lay.geom; L->many = nullptr;
     L->asym = 0;
     L->rowsum = (int32_t*)(L->prepared + lay.rowsum);
     if (L->rot) {
-        st = launch_prepare_rot(L->geom, P1, P2, prepared, (cudaStream_t)stream);
-        if (st == BWLA_OK && lay.has_rows) st = launch_prepare_rows(lay.rows_geom, P1, P2, L->many, (cudaStream_t)stream);
-        if (st == BWLA_OK && lay.has_okt) st = launch_prepare_okt(lay.okt_geom, P1, P2, L->many, (cudaStream_t)stream);
+        PreparedFactors f;
+        st = prepare_factors(n1, n2, P1, P2, L->prepared, &f, (cudaStream_t)stream);
         if (st != BWLA_OK) { free(L); return st; }
+        L->many = f.many;
     }
     st = launch_row_sums(packed, N, K, L->rowsum, (cudaStream_t)stream);
     if (st != BWLA_OK) { free(L); return st; }

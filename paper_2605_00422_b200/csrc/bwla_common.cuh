@@ -114,6 +114,10 @@ int validate_linear_call(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, 
                          const void* V_bf16, int r, const void* out_bf16, int64_t N, int64_t ldo, const void* workspace,
                          size_t workspace_bytes);
 
+// BWLA_OK where an sm_100 device is current
+int check_device();
+bool valid_rotation_dims(int64_t K, int n1, int n2);
+
 // ---------------------------------------------------------------------------------------------
 // kernel launchers (each returns a BWLA status; all asynchronous on `stream`)
 // ---------------------------------------------------------------------------------------------
@@ -205,6 +209,16 @@ int launch_rot_binarize(const RotGeom& g, const void* w, int dtype, int64_t N, i
 // qsum[t][0] = sum_k codes[t][k] (the other parts zero); optionally rewrites natural-order codes into the interleaved order.
 int launch_prepare_codes(const int8_t* codes, int64_t M, int64_t K, int8_t* codes_interleaved, int32_t* qsum,
                          cudaStream_t stream);
+
+// The Kronecker factors of a prepared layer in the forms that the rotation kernels read, in caller's memory of prepared_factor_bytes
+// (factors that rot_geometry takes).
+struct PreparedFactors {
+    RotGeom geom;
+    const uint8_t* base;      // RotProblem::prepared
+    uint8_t* many;            // RotProblem::many
+};
+size_t prepared_factor_bytes(int n1, int n2);
+int prepare_factors(int n1, int n2, const float* P1, const float* P2, uint8_t* prepared, PreparedFactors* out, cudaStream_t stream);
 
 struct GemmArgs {
     const int8_t* codes;      // [M][K]; natural order for the simple path

@@ -5,6 +5,7 @@
 // whichever build of the library the process has loaded is the one that is called.  As through ctypes, other threads run while the
 // library works, and what PyTorch throws (a tensor without memory of its own, a stream of a device that is not there) becomes a Python
 // exception.
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -18,12 +19,16 @@ struct Entry {
     decltype(&bwla_w1ax_linear) linear;
     decltype(&bwla_layer_w1a16_linear) a16;
     decltype(&bwla_pack_signs) pack;
+    decltype(&bwla_fp4_quantize_rows) fp4_quantize;
+    decltype(&bwla_fp4_expand_rows) fp4_expand;
+    decltype(&bwla_fp4_gemm_codes) fp4_gemm;
+    decltype(&bwla_fp4_layer_linear) fp4_linear;
 } entry;
 
-PyObject *name_handle, *name_n, *name_k;      // of a layer: "_h", its handle as an integer; "N", "K"
+PyObject *name_handle, *name_fp4, *name_n, *name_k;      // of a layer: "_h" or "_fp4", its handle as an integer; "N", "K"
 
 const char* dtype_name(at::ScalarType t) {
-    return t == at::kBFloat16 ? "torch.bfloat16" : t == at::kFloat ? "torch.float32" : t == at::kInt ? "torch.int32" : "another type";
+    return t == at::kBFloat16 ? "torch.bfloat16" : t == at::kFloat ? "torch.float32" : t == at::kInt ? "torch.int32" : t == at::kByte ? "torch.uint8" : "another type";
 }
 
 // The tensor behind `o` when it is a CUDA tensor of this type (and number of dimensions), else NULL with TypeError set.
@@ -176,14 +181,144 @@ PyObject* call_pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- microscaled 4-bit rows: codes [rows][K/2], scale tiles, row scales (or None) ----
+struct Fp4Rows {
+    int64_t rows = 0, K = 0;
+    void *codes = nullptr, *scales = nullptr, *row_scales = nullptr;
+};
+// The library works on the current device: tensors of another one are refused.
+bool here(const at::Tensor& t, const char* name) {
+    if (t.is_cuda() && t.device().index() == c10::cuda::current_device()) return true;
+    PyErr_Format(PyExc_TypeError, "%s: expected a tensor of the current CUDA device", name);
+    return false;
+}
+// tensors that are long enough for their rows: the library sees pointers only
+bool fp4_rows(PyObject* codes, PyObject* scales, PyObject* row_scales, int format, const char* names[3], Fp4Rows* out) {
+    const at::Tensor *c = need(codes, at::kByte, names[0], 2), *s, *r = nullptr;
+    if (!c || !(s = need(scales, at::kByte, names[1], 1)) || (row_scales != Py_None && !(r = need(row_scales, at::kFloat, names[2], 1)))) return false;
+    out->rows = c->size(0);
+    out->K = 2 * c->size(1);
+    const int64_t block = format == BWLA_FP4_NV ? 16 : 32;
+    if (!c->is_contiguous() || s->numel() < (out->rows + 127) / 128 * ((out->K / block + 3) / 4) * 512 || (r && r->numel() < out->rows)) {
+        PyErr_Format(PyExc_TypeError, "%s must be contiguous, %s and %s long enough for its rows", names[0], names[1], names[2]);
+        return false;
+    }
+    if (!here(*c, names[0]) || !here(*s, names[1]) || (r && !here(*r, names[2]))) return false;
+    out->codes = c->data_ptr();
+    out->scales = s->data_ptr();
+    out->row_scales = r ? r->data_ptr() : nullptr;
+    return true;
+}
+bool fp4_format(PyObject* o, int* format) {
+    const long v = PyLong_AsLong(o);
+    if (v == -1 && PyErr_Occurred()) return false;
+    *format = v == BWLA_FP4_MX || v == BWLA_FP4_NV ? (int)v : -1;      // (what is neither is refused by the library)
+    return true;
+}
+int float_dtype(const at::Tensor& t) {
+    return t.scalar_type() == at::kFloat ? BWLA_DTYPE_F32 : t.scalar_type() == at::kBFloat16 ? BWLA_DTYPE_BF16 : t.scalar_type() == at::kHalf ? BWLA_DTYPE_F16 : -1;
+}
+
+// fp4_quantize(x, format, codes, scales, row_scales) -> status
+PyObject* call_fp4_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "fp4_quantize(x, format, codes, scales, row_scales)"); return nullptr; }
+    static const char* names[3] = {"codes", "scales", "row_scales"};
+    const at::Tensor* x = tensor(args[0], "x");
+    int format;
+    Fp4Rows q;
+    if (!x) return nullptr;
+    if (float_dtype(*x) < 0) { PyErr_SetString(PyExc_TypeError, "x must be fp32, bf16 or fp16"); return nullptr; }
+    if (!need(args[0], x->scalar_type(), "x", 2) || !here(*x, "x") || !fp4_format(args[1], &format) || !fp4_rows(args[2], args[3], args[4], format, names, &q)) return nullptr;
+    const int64_t M = x->size(0), K = x->size(1);
+    if (q.rows != M || q.K != K) { PyErr_SetString(PyExc_TypeError, "codes must be [M][K/2] for x of [M][K]"); return nullptr; }
+    return unlocked(entry.fp4_quantize, (const void*)x->data_ptr(), float_dtype(*x), M, K, M > 0 ? x->stride(0) : K, format, (uint8_t*)q.codes, (uint8_t*)q.scales,
+                    (float*)q.row_scales, stream());
+    END_HANDLE_TH_ERRORS
+}
+
+// fp4_expand(codes, scales, row_scales, format, out) -> status
+PyObject* call_fp4_expand(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "fp4_expand(codes, scales, row_scales, format, out)"); return nullptr; }
+    static const char* names[3] = {"codes", "scales", "row_scales"};
+    int format;
+    Fp4Rows q;
+    const at::Tensor* out = tensor(args[4], "out");
+    if (!out || !fp4_format(args[3], &format) || !fp4_rows(args[0], args[1], args[2], format, names, &q)) return nullptr;
+    if (float_dtype(*out) != BWLA_DTYPE_F32 && float_dtype(*out) != BWLA_DTYPE_BF16) { PyErr_SetString(PyExc_TypeError, "out must be fp32 or bf16"); return nullptr; }
+    if (!need(args[4], out->scalar_type(), "out", 2) || !here(*out, "out")) return nullptr;
+    if (out->size(0) != q.rows || out->size(1) != q.K) { PyErr_SetString(PyExc_TypeError, "out must be [M][K] for codes of [M][K/2]"); return nullptr; }
+    return unlocked(entry.fp4_expand, (const uint8_t*)q.codes, (const uint8_t*)q.scales, (const float*)q.row_scales, q.rows, q.K, format, out->data_ptr(),
+                    float_dtype(*out), q.rows > 0 ? out->stride(0) : q.K, stream());
+    END_HANDLE_TH_ERRORS
+}
+
+// fp4_gemm(a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, format, out, workspace) -> status
+PyObject* call_fp4_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    if (nargs != 9) { PyErr_SetString(PyExc_TypeError, "fp4_gemm: nine arguments"); return nullptr; }
+    static const char *a_names[3] = {"a_codes", "a_scales", "a_rows"}, *w_names[3] = {"w_codes", "w_scales", "w_rows"};
+    int format;
+    Fp4Rows a, w;
+    const at::Tensor *out, *ws;
+    if (!fp4_format(args[6], &format) || !fp4_rows(args[0], args[1], args[2], format, a_names, &a) || !fp4_rows(args[3], args[4], args[5], format, w_names, &w) ||
+        !(out = need(args[7], at::kBFloat16, "out", 2)) || !here(*out, "out") || !(ws = tensor(args[8], "workspace")) || !here(*ws, "workspace"))
+        return nullptr;
+    if (a.K != w.K || out->size(0) != a.rows || out->size(1) != w.rows) {
+        PyErr_SetString(PyExc_TypeError, "a_codes [M][K/2], w_codes [N][K/2] and out [M][N] do not fit");
+        return nullptr;
+    }
+    return unlocked(entry.fp4_gemm, (const uint8_t*)a.codes, (const uint8_t*)a.scales, (const float*)a.row_scales, a.rows, a.K, (const uint8_t*)w.codes,
+                    (const uint8_t*)w.scales, (const float*)w.row_scales, w.rows, format, out->data_ptr(), a.rows > 0 ? out->stride(0) : w.rows, ws->data_ptr(),
+                    (size_t)ws->nbytes(), stream());
+    END_HANDLE_TH_ERRORS
+}
+
+// fp4_linear(layer, x, out, workspace) -> status
+PyObject* call_fp4_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    if (nargs != 4) { PyErr_SetString(PyExc_TypeError, "fp4_linear(layer, x, out, workspace)"); return nullptr; }
+    const at::Tensor *x = need(args[1], at::kBFloat16, "x", 2), *out, *ws;
+    if (!x || !here(*x, "x") || !(out = need(args[2], at::kBFloat16, "out", 2)) || !here(*out, "out") || !(ws = tensor(args[3], "workspace")) || !here(*ws, "workspace"))
+        return nullptr;
+    PyObject* o = PyObject_GetAttr(args[0], name_fp4);
+    if (!o) return nullptr;
+    Ref h(o);
+    const bwla_fp4_layer* layer = o == Py_None ? nullptr : (const bwla_fp4_layer*)PyLong_AsVoidPtr(o);
+    int64_t K, N;
+    if (PyErr_Occurred() || !size_of(args[0], name_k, &K) || !size_of(args[0], name_n, &N)) return nullptr;
+    const int64_t M = x->size(0);
+    if (x->size(1) != K || out->size(0) != M || out->size(1) != N) { PyErr_SetString(PyExc_TypeError, "x must be [M][K] and out [M][N] of the layer"); return nullptr; }
+    return unlocked(entry.fp4_linear, layer, (const void*)x->data_ptr(), M, M > 0 ? x->stride(0) : K, out->data_ptr(), M > 0 ? out->stride(0) : N, ws->data_ptr(),
+                    (size_t)ws->nbytes(), stream());
+    END_HANDLE_TH_ERRORS
+}
+
+bool addresses(PyObject* const* args, void* (&p)[4]) {
+    for (int i = 0; i < 4; ++i) {
+        p[i] = PyLong_AsVoidPtr(args[i]);
+        if (!p[i]) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: null address"); return false; }
+    }
+    return true;
+}
+// bind_fp4(quantize, expand, gemm, linear): as bind
+PyObject* bind_fp4(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 4) { PyErr_SetString(PyExc_TypeError, "bind_fp4: four addresses"); return nullptr; }
+    void* p[4];
+    if (!addresses(args, p)) return nullptr;
+    entry.fp4_quantize = (decltype(entry.fp4_quantize))p[0];
+    entry.fp4_expand = (decltype(entry.fp4_expand))p[1];
+    entry.fp4_gemm = (decltype(entry.fp4_gemm))p[2];
+    entry.fp4_linear = (decltype(entry.fp4_linear))p[3];
+    Py_RETURN_NONE;
+}
+
 // bind(group, linear, a16, pack): the library's entry points as addresses
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 4) { PyErr_SetString(PyExc_TypeError, "bind: four addresses"); return nullptr; }
     void* p[4];
-    for (int i = 0; i < 4; ++i) {
-        p[i] = PyLong_AsVoidPtr(args[i]);
-        if (!p[i]) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: null address"); return nullptr; }
-    }
+    if (!addresses(args, p)) return nullptr;
     entry.group = (decltype(entry.group))p[0];
     entry.linear = (decltype(entry.linear))p[1];
     entry.a16 = (decltype(entry.a16))p[2];
@@ -193,6 +328,11 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
+    {"bind_fp4", (PyCFunction)(void (*)(void))bind_fp4, METH_FASTCALL, nullptr},
+    {"fp4_quantize", (PyCFunction)(void (*)(void))call_fp4_quantize, METH_FASTCALL, nullptr},
+    {"fp4_expand", (PyCFunction)(void (*)(void))call_fp4_expand, METH_FASTCALL, nullptr},
+    {"fp4_gemm", (PyCFunction)(void (*)(void))call_fp4_gemm, METH_FASTCALL, nullptr},
+    {"fp4_linear", (PyCFunction)(void (*)(void))call_fp4_linear, METH_FASTCALL, nullptr},
     {"group", (PyCFunction)(void (*)(void))call_group, METH_FASTCALL, nullptr},
     {"a16", (PyCFunction)(void (*)(void))call_a16, METH_FASTCALL, nullptr},
     {"linear", (PyCFunction)(void (*)(void))call_linear, METH_FASTCALL, nullptr},
@@ -204,7 +344,8 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods,
 
 PyMODINIT_FUNC PyInit__calls(void) {
     name_handle = PyUnicode_InternFromString("_h");
+    name_fp4 = PyUnicode_InternFromString("_fp4");
     name_n = PyUnicode_InternFromString("N");
     name_k = PyUnicode_InternFromString("K");
-    return name_handle && name_n && name_k ? PyModule_Create(&module_def) : nullptr;
+    return name_handle && name_fp4 && name_n && name_k ? PyModule_Create(&module_def) : nullptr;
 }

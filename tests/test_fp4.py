@@ -1,0 +1,111 @@
+"""Microscaled 4-bit floating point without a GPU: the oracle against the formats' own numbers, sizes, refusals."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import fp4
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2605_00422_b200 import bwla
+    return bwla._lib
+
+
+def test_oracle_rounds_as_the_formats_say():
+    assert fp4.E4M3[-1] == 448 and fp4.E4M3[1] == 2.0 ** -9
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.9, 1e9])
+    assert fp4.E2M1[fp4.nearest(ties, fp4.E2M1)].tolist() == [0, 1, 1, 2, 2, 4, 4, 6, 6]
+    up = np.nextafter(ties, np.inf)
+    assert fp4.E2M1[fp4.nearest(up, fp4.E2M1)].tolist() == [.5, 1, 1.5, 2, 3, 4, 6, 6, 6]
+    # the scale of a block: the largest value lands in [4, 8)
+    for top in (1.0, 1.99, 2.0, 6.0, 7.9, 8.0, 3e38, 2.0 ** -149):
+        e = int(fp4.mx_exponent(np.float64(top)))
+        assert (4 <= top / 2.0 ** e < 8) or e == -127
+    # the scale of a row: the smallest power of two that brings the largest block's scale into e4m3's range
+    for top in (2688.0, 2688.0001, 2687.9, 1.0, 1e-30, 3e38):
+        E = int(fp4.nv_exponent(np.float64(top)))
+        assert top <= 2688 * 2.0 ** E and top > 2688 * 2.0 ** (E - 1)
+    v, s, r = fp4.quantize(np.array([[0.0] * 16 + [2688.0] * 8 + [1.0] * 8]), "nv")
+    assert r[0] == 1 and s[0].tolist() == [0, 448] and v[0, 16] == 6 and v[0, -1] == 0
+    for fmt in ("mx", "nv"):
+        x = np.random.default_rng(1).standard_normal((3, 96))
+        x[1, 40] = np.nan
+        v, s, r = fp4.quantize(x, fmt)
+        y = fp4.expand(v, s, r, fmt)
+        assert np.isnan(y[1, 32:64]).all() and np.isnan(y[1]).all() == (fmt == "nv") and np.isfinite(y[[0, 2]]).all()
+        assert np.array_equal(fp4.unpack(fp4.pack(v)), v)
+        b = fp4.scale_bytes(s, fmt)
+        assert np.array_equal(fp4.untile(fp4.tile(b), 3, b.shape[1]), b)
+        assert np.array_equal(fp4.scales_of(b, fmt), s, equal_nan=True)
+
+
+@pytest.mark.parametrize("rows,K,format,want", [(1, 32, 0, 512), (128, 128, 0, 512), (129, 160, 0, 2048), (1, 64, 1, 512), (333, 11008, 1, 3 * 172 * 512),
+                                                 (0, 32, 0, 0), (1, 48, 0, 0), (1, 0, 0, 0), (-1, 32, 0, 0), (1, 32, 2, 0), (1, 1 << 25, 0, 0)])
+def test_scale_bytes(lib, rows, K, format, want):
+    assert lib.bwla_fp4_scale_bytes(rows, K, format) == want
+
+
+def test_refusals_before_anything_runs(lib):
+    """Bad arguments are refused before the device is looked at; good ones end at the missing device (here) or are not made."""
+    buf = (C.c_uint8 * 4096)()
+    at = (C.addressof(buf) + 255) // 256 * 256
+    p, odd = C.c_void_p(at), C.c_void_p(at + 8)
+    bad = -1
+    q = lambda **k: lib.bwla_fp4_quantize_rows(*[{**dict(x=p, dtype=0, M=1, K=32, ldx=32, format=0, codes=p, scales=p, rows=p), **k}[n]
+                                                for n in ("x", "dtype", "M", "K", "ldx", "format", "codes", "scales", "rows")], None)
+    for k in (dict(x=None), dict(dtype=3), dict(dtype=-1), dict(M=-1), dict(K=0), dict(K=33), dict(K=16), dict(K=1 << 25, ldx=1 << 25), dict(ldx=31), dict(format=2),
+              dict(codes=None), dict(codes=odd), dict(scales=None), dict(scales=odd), dict(format=1, rows=None), dict(M=1 << 31)):
+        assert q(**k) == bad, k
+    assert q(M=0, x=None, codes=None) == 0
+    e = lambda **k: lib.bwla_fp4_expand_rows(*[{**dict(codes=p, scales=p, rows=None, M=1, K=32, format=0, out=p, dtype=1, ldo=32), **k}[n]
+                                              for n in ("codes", "scales", "rows", "M", "K", "format", "out", "dtype", "ldo")], None)
+    for k in (dict(codes=None), dict(scales=None), dict(out=None), dict(dtype=2), dict(ldo=31), dict(K=24), dict(format=-1), dict(M=-1), dict(codes=odd)):
+        assert e(**k) == bad, k
+    assert e(M=0) == 0
+    names = ("ac", "as_", "ar", "M", "K", "wc", "ws", "wr", "N", "format", "out", "ldo", "work", "bytes")
+    good = dict(ac=p, as_=p, ar=None, M=1, K=32, wc=p, ws=p, wr=None, N=8, format=0, out=p, ldo=8, work=p, bytes=256)
+    g = lambda **k: lib.bwla_fp4_gemm_codes(*[{**good, **k}[n] for n in names], None)
+    for k in (dict(ac=None), dict(as_=None), dict(wc=None), dict(ws=None), dict(out=None), dict(ldo=7), dict(K=31), dict(M=-1), dict(N=-1), dict(format=5), dict(ac=odd),
+              dict(wc=odd), dict(as_=odd), dict(ws=odd), dict(out=C.c_void_p(at + 1))):
+        assert g(**k) == bad, k
+    for k in (dict(work=None), dict(work=odd), dict(bytes=255)):
+        assert g(**k) == -3, k
+    assert g(M=0) == 0 and g(N=0) == 0
+    assert lib.bwla_fp4_gemm_workspace_bytes(1, 32, 8) >= 256 and lib.bwla_fp4_gemm_workspace_bytes(1, 33, 8) == 0
+    r = lambda **k: lib.bwla_rotate_quant_fp4(*[{**dict(x=p, M=1, K=64, ldx=64, P1=p, n1=8, P2=p, n2=8, format=0, codes=p, scales=p, rows=p, work=p, bytes=1 << 20), **k}[n]
+                                               for n in ("x", "M", "K", "ldx", "P1", "n1", "P2", "n2", "format", "codes", "scales", "rows", "work", "bytes")], None)
+    for k in (dict(x=None), dict(K=96), dict(n1=9), dict(ldx=63), dict(P1=None), dict(P2=odd), dict(codes=odd), dict(format=1, rows=None), dict(M=-1), dict(format=2)):
+        assert r(**k) == bad, k
+    assert r(work=None) == -3 and r(bytes=255) == -3 and r(M=0) == 0
+    h = C.c_void_p()
+    c = lambda **k: lib.bwla_fp4_layer_create(C.byref(h), *[{**dict(K=64, N=8, P1=p, n1=8, P2=p, n2=8, format=0, wc=p, ws=p, wr=None, prepared=p, bytes=1 << 20), **k}[n]
+                                              for n in ("K", "N", "P1", "n1", "P2", "n2", "format", "wc", "ws", "wr", "prepared", "bytes")], None)
+    for k in (dict(K=96), dict(N=0), dict(P1=None), dict(wc=None), dict(ws=odd), dict(format=9), dict(n2=4)):
+        assert c(**k) == bad, k
+    assert c(prepared=None) == -3 and c(bytes=16) == -3
+    assert lib.bwla_fp4_layer_linear(None, p, 1, 64, p, 8, p, 256, None) == bad
+    assert lib.bwla_fp4_layer_rotate_quant(None, p, 1, 64, p, p, p, p, 256, None) == bad
+    assert lib.bwla_fp4_layer_workspace_bytes(None, 1) == 0 and lib.bwla_fp4_layer_prepared_bytes(65, 8, 8) == 0
+    import torch
+    if not torch.cuda.is_available():
+        assert q() == e() == g() == r() == c() == -2          # BWLA_ERR_UNSUPPORTED: nothing ran
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    """Shapes and types: TypeError before a pointer is taken (tensors here are on the CPU, or of the wrong kind)."""
+    import torch
+
+    from paper_2605_00422_b200 import bwla
+    x = torch.zeros(2, 64)
+    for call in (lambda: bwla.bwla_fp4_quantize_rows(x, 0), lambda: bwla.bwla_fp4_expand_rows(torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), None, 0),
+                 lambda: bwla.bwla_fp4_gemm_codes(x, x, None, x, x, None, 0, out=x, workspace=x), lambda: bwla.bwla_rotate_quant_fp4(x, x, x, 0, workspace=x),
+                 lambda: bwla.bwla_fp4_quantize_rows(x.double(), 0)):
+        with pytest.raises((TypeError, RuntimeError)):
+            call()
+
+    class Other:
+        _h, N, K = 1, 64, 64
+    with pytest.raises((AttributeError, TypeError)):
+        bwla._calls.fp4_linear(Other(), x.bfloat16(), x.bfloat16(), x)
