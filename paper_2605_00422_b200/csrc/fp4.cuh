@@ -5,6 +5,7 @@
 // tiles of 128 rows x 4 blocks, the 512 bytes that tcgen05.cp (32x128b) brings to tensor memory as tcgen05.mma wants them.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <stdint.h>
@@ -134,5 +135,10 @@ struct Fp4GemmArgs {
     uint32_t* status;
 };
 int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream);
+
+// The maps of an operand: its codes as boxes of `box_rows` rows x 256 values (128 bytes, 128-byte swizzle), its scale tiles as boxes of
+// `tile_rows` x 128 rows x 256 values.
+struct Fp4Maps { CUtensorMap a, a_scales, w, w_scales; };
+int fp4_operand_maps(CUtensorMap* codes, CUtensorMap* scales, const uint8_t* c, const uint8_t* s, int64_t rows, int64_t K, int format, int box_rows, int tile_rows);
 
 }  // namespace bwla

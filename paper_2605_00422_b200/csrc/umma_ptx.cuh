@@ -402,6 +402,43 @@ __device__ __forceinline__ uint64_t smem_desc_mnmajor64(uint32_t smem_addr, uint
     return d;
 }
 
+// ---- block-scaled 4-bit MMAs (kind::mxf4: e8m0 scales of 32 values, kind::mxf4nvf4: e4m3 scales of 16) ----
+// 512 bytes of scales (128 rows x 4, row r at 16 (r % 32) + 4 (r / 32)) from shared memory into four columns, the same in all lane quarters:
+// lane l of column c has the four scales of row 32 c + l.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t smem_addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(128 >> 4) << 32;                                // 8 rows of 16 bytes to the next
+    d |= (uint64_t)1 << 46;
+    return d;
+}
+template <bool PAIR>
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t desc) {
+    if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// D[tmem] (+)= (A * scales) (B * scales)^T over 64 values of k, both operands K-major in shared memory.
+template <bool PAIR, bool NV>
+__device__ __forceinline__ void mma_fp4_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa_tmem, uint32_t sfb_tmem,
+                                           uint32_t accumulate) {
+#define BWLA_FP4_MMA(GROUP, KIND)                                                                                           \
+    asm volatile(                                                                                                           \
+        "{\n\t.reg .pred p;\n\t"                                                                                            \
+        "setp.ne.b32 p, %4, 0;\n\t"                                                                                         \
+        "tcgen05.mma.cta_group::" GROUP "." KIND " [%0], %1, %2, %3, [%5], [%6], p;\n\t}"                                    \
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(sfa_tmem), "r"(sfb_tmem)                   \
+        : "memory")
+    if constexpr (PAIR && NV) BWLA_FP4_MMA("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else if constexpr (PAIR) BWLA_FP4_MMA("2", "kind::mxf4.block_scale.scale_vec::2X");
+    else if constexpr (NV) BWLA_FP4_MMA("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else BWLA_FP4_MMA("1", "kind::mxf4.block_scale.scale_vec::2X");
+#undef BWLA_FP4_MMA
+}
+// Instruction descriptor: e2m1 x e2m1, `rows` x `cols`, scales e4m3 or e8m0; `id`: first of the two (kind::mxf4) bytes of a scale cell.
+__device__ __forceinline__ constexpr uint32_t idesc_fp4(int rows, int cols, bool nv, int id) {
+    return (uint32_t)id << 4 | 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (nv ? 0u : 1u) << 23 | (uint32_t)(rows >> 4) << 24 | (uint32_t)id << 29;
+}
+
 // D[tmem] (+)= A[tmem] * B[smem descriptor], bf16 x bf16 -> fp32 (A: 128 lanes, two bf16 per 32-bit column).
 __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
                                            uint32_t accumulate) {
