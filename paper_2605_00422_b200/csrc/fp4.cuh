@@ -54,6 +54,12 @@ __device__ __forceinline__ void fp4_values8(uint32_t codes, float (&v)[8]) {
     }
 }
 
+__device__ __forceinline__ uint32_t cvt_pair(float lo, float hi) {      // two bf16, rounded to nearest
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
 __device__ __forceinline__ uint32_t fp4_e4m3(float v) {              // to nearest even, beyond 448 to 448
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(r) : "f"(v), "f"(0.f));
@@ -135,6 +141,7 @@ struct Fp4GemmArgs {
     uint32_t* status;
 };
 int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream);
+int launch_fp4_pair(const Fp4GemmArgs& a, cudaStream_t stream);
 
 // The maps of an operand: its codes as boxes of `box_rows` rows x 256 values (128 bytes, 128-byte swizzle), its scale tiles as boxes of
 // `tile_rows` x 128 rows x 256 values.

@@ -206,10 +206,7 @@ __global__ void __launch_bounds__(fp4_split::kThreads, 2) fp4_split_kernel(const
         const float ar = p.a_rows ? __ldg(p.a_rows + t0 + t) : 1.f;
         __nv_bfloat16* o = p.out + (int64_t)(t0 + t) * p.ldo + n;
         if (p.vec && n + 3 < p.N) {
-            uint2 w;
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(v[1] * ar * wr[1]), "f"(v[0] * ar * wr[0]));
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(v[3] * ar * wr[3]), "f"(v[2] * ar * wr[2]));
-            *reinterpret_cast<uint2*>(o) = w;
+            *reinterpret_cast<uint2*>(o) = make_uint2(cvt_pair(v[0] * ar * wr[0], v[1] * ar * wr[1]), cvt_pair(v[2] * ar * wr[2], v[3] * ar * wr[3]));
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -272,6 +269,8 @@ static int launch_format(const Fp4GemmArgs& a, cudaStream_t stream) {
                                                                                                              : launch_split<NV, 128>(a, stream);
 }
 int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream) {
+    static const int force = getenv("FP4_FORCE") ? atoi(getenv("FP4_FORCE")) : 0;
+    if (force ? force == 2 : a.M > 256) return launch_fp4_pair(a, stream);
     return a.format == BWLA_FP4_NV ? launch_format<true>(a, stream) : launch_format<false>(a, stream);
 }
 
