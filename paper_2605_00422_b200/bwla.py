@@ -439,25 +439,23 @@ def _fp4_outputs(rows: int, K: int, format: int, device):
 def bwla_fp4_quantize_rows(x: torch.Tensor, format: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                            row_scales: Optional[torch.Tensor] = None):
     """x: fp32, bf16 or fp16 [M][K] (row stride >= K) -> (codes uint8 [M][K/2], scale tiles uint8, row scales fp32 [M] or None)."""
-    if codes is None or scales is None or (row_scales is None and format == BWLA_FP4_NV):
-        made = _fp4_outputs(x.shape[0], x.shape[-1], format, x.device)
-        codes, scales = made[0] if codes is None else codes, made[1] if scales is None else scales
-        row_scales = made[2] if row_scales is None else row_scales
-    st = _calls.fp4_quantize(x, format, codes, scales, row_scales)
-    if st:
-        _check(st, "bwla_fp4_quantize_rows")
-    return codes, scales, row_scales
+    made = _calls.fp4_quantize(x, format, codes, scales, row_scales)
+    if type(made) is int:
+        _check(made, "bwla_fp4_quantize_rows")
+    return made
 
 
 def bwla_fp4_expand_rows(codes: torch.Tensor, scales: torch.Tensor, row_scales: Optional[torch.Tensor], format: int,
                          out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
     """The values [M][K] (bf16, or fp32) that quantised rows stand for."""
     if out is None:
-        out = torch.empty((codes.shape[0], 2 * codes.shape[-1]), dtype=dtype, device=codes.device)
-    st = _calls.fp4_expand(codes, scales, row_scales, format, out)
-    if st:
-        _check(st, "bwla_fp4_expand_rows")
-    return out
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError("dtype must be bf16 or fp32")
+        out = 0 if dtype is torch.bfloat16 else 1
+    made = _calls.fp4_expand(codes, scales, row_scales, format, out)
+    if type(made) is int:
+        _check(made, "bwla_fp4_expand_rows")
+    return made
 
 
 def bwla_fp4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
@@ -476,14 +474,12 @@ def bwla_fp4_gemm_codes(a_codes: torch.Tensor, a_scales: torch.Tensor, a_rows: O
                         w_scales: torch.Tensor, w_rows: Optional[torch.Tensor], format: int, out: Optional[torch.Tensor] = None,
                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Product of quantised rows [M][K] and [N][K] (codes, scale tiles, row scales or None each): bf16 out [M][N]."""
-    if out is None:
-        out = torch.empty((a_codes.shape[0], w_codes.shape[0]), dtype=torch.bfloat16, device=a_codes.device)
     if workspace is None:
         workspace = new_fp4_workspace(a_codes.shape[0], 2 * a_codes.shape[-1], w_codes.shape[0], a_codes.device)
-    st = _calls.fp4_gemm(a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, format, out, workspace)
-    if st:
-        _check(st, "bwla_fp4_gemm_codes")
-    return out
+    made = _calls.fp4_gemm(a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, format, out, workspace)
+    if type(made) is int:
+        _check(made, "bwla_fp4_gemm_codes")
+    return made
 
 
 def bwla_rotate_quant_fp4_workspace_bytes(M: int, K: int) -> int:
@@ -582,14 +578,12 @@ def new_fp4_layer_workspace(layer: Fp4Layer, M: int, device="cuda") -> torch.Ten
 def bwla_fp4_layer_linear(layer: Fp4Layer, x: torch.Tensor, out: Optional[torch.Tensor] = None,
                           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The prepared 4-bit layer: bf16 x [M][K] -> bf16 out [M][N]."""
-    if out is None:
-        out = torch.empty((x.shape[0], layer.N), dtype=torch.bfloat16, device=x.device)
     if workspace is None:
         workspace = new_fp4_layer_workspace(layer, x.shape[0], x.device)
-    st = _calls.fp4_linear(layer, x, out, workspace)
-    if st:
-        _check(st, "bwla_fp4_layer_linear")
-    return out
+    made = _calls.fp4_linear(layer, x, out, workspace)
+    if type(made) is int:
+        _check(made, "bwla_fp4_layer_linear")
+    return made
 
 
 def _handles(layers):

@@ -236,8 +236,15 @@ static int launch_split(const Fp4GemmArgs& a, cudaStream_t stream) {
     p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + kBlockK - 1) / kBlockK);
     p.once = tok_tiles == 1; p.a_rows = a.a_rows; p.w_rows = a.w_rows; p.out = a.out; p.ldo = a.ldo; p.status = a.status;
     p.vec = (reinterpret_cast<uintptr_t>(a.out) & 7) == 0 && a.ldo % 4 == 0;
-    const int64_t room = 2 * (int64_t)std::max(1, sm_count()) / (row_tiles * tok_tiles);
-    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(room, kMaxSplit), p.kblocks));
+    // How many CTAs K is cut over.  One an SM leaves room for the kernel behind this one to start beside it (its weights are on their way when
+    // this one ends); more pay where each still has four k-blocks, and up to 13 for 8 SMs clusters of any size fit at once.  In a chain of
+    // calls, us, parts 1 | 2 | 3 | 4 | 5 | 6 | 7 | 8:  5120 x 5120, 1 token 6.6 5.4 5.3 5.1 5.1 5.2 9.1 8.5;  4096 x 4096 5.3 4.5 4.5 4.2 4.5 4.5 5.0 4.9;
+    // 25600 -> 5120, 64 tokens 33 21 17.3 16.1 15.4 15.1 23.4 22.1;  4096 -> 11008, 16 tokens 6.9 6.5 7.0 10.7 ...;  25600 -> 1024, 1 token 23 13.4 10.2
+    // 8.3 7.6 6.8 6.8 6.4.
+    const int64_t sms = std::max(1, sm_count()), tiles = row_tiles * tok_tiles;
+    int64_t cut = std::min<int64_t>(std::min<int64_t>(kMaxSplit, p.kblocks), 13 * sms / 8 / tiles);
+    if (cut * tiles > sms && 4 * cut > p.kblocks) cut = std::max<int64_t>(sms / tiles, p.kblocks / 4);
+    const int parts = (int)std::max<int64_t>(1, cut);
     static thread_local int configured = -1;
     int dev = 0;
     BWLA_CUDA_TRY(cudaGetDevice(&dev));

@@ -5,6 +5,7 @@
 // whichever build of the library the process has loaded is the one that is called.  As through ctypes, other threads run while the
 // library works, and what PyTorch throws (a tensor without memory of its own, a stream of a device that is not there) becomes a Python
 // exception.
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -82,6 +83,7 @@ struct Ref {
     explicit Ref(PyObject* p) : o(p) {}
     ~Ref() { Py_XDECREF(o); }
     Ref(const Ref&) = delete;
+    Ref(Ref&& other) noexcept : o(other.o) { other.o = nullptr; }
 };
 
 // group(layers, x, outs, workspace) -> status
@@ -219,7 +221,16 @@ int float_dtype(const at::Tensor& t) {
     return t.scalar_type() == at::kFloat ? BWLA_DTYPE_F32 : t.scalar_type() == at::kBFloat16 ? BWLA_DTYPE_BF16 : t.scalar_type() == at::kHalf ? BWLA_DTYPE_F16 : -1;
 }
 
-// fp4_quantize(x, format, codes, scales, row_scales) -> status
+// What a call returns: the status where it is not 0, else its outputs.
+PyObject* fp4_result(PyObject* status, PyObject* outputs) {
+    if (!status || !outputs) { Py_XDECREF(status); Py_XDECREF(outputs); return nullptr; }
+    if (PyLong_AsLong(status) != 0) { Py_DECREF(outputs); return status; }
+    Py_DECREF(status);
+    return outputs;
+}
+Ref fp4_new(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& like) { return Ref(THPVariable_Wrap(at::empty(sizes, like.options().dtype(type)))); }
+
+// fp4_quantize(x, format, codes, scales, row_scales) -> (codes, scales, row_scales), those that are None made here, or status
 PyObject* call_fp4_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
     if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "fp4_quantize(x, format, codes, scales, row_scales)"); return nullptr; }
@@ -229,32 +240,40 @@ PyObject* call_fp4_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
     Fp4Rows q;
     if (!x) return nullptr;
     if (float_dtype(*x) < 0) { PyErr_SetString(PyExc_TypeError, "x must be fp32, bf16 or fp16"); return nullptr; }
-    if (!need(args[0], x->scalar_type(), "x", 2) || !here(*x, "x") || !fp4_format(args[1], &format) || !fp4_rows(args[2], args[3], args[4], format, names, &q)) return nullptr;
+    if (!need(args[0], x->scalar_type(), "x", 2) || !here(*x, "x") || !fp4_format(args[1], &format)) return nullptr;
     const int64_t M = x->size(0), K = x->size(1);
-    if (q.rows != M || q.K != K) { PyErr_SetString(PyExc_TypeError, "codes must be [M][K/2] for x of [M][K]"); return nullptr; }
-    return unlocked(entry.fp4_quantize, (const void*)x->data_ptr(), float_dtype(*x), M, K, M > 0 ? x->stride(0) : K, format, (uint8_t*)q.codes, (uint8_t*)q.scales,
-                    (float*)q.row_scales, stream());
+    const Ref codes = args[2] != Py_None ? Ref(Py_NewRef(args[2])) : fp4_new({M, K / 2}, at::kByte, *x);
+    const Ref scales = args[3] != Py_None ? Ref(Py_NewRef(args[3])) : fp4_new({(M + 127) / 128 * ((K / (format == BWLA_FP4_NV ? 16 : 32) + 3) / 4) * 512}, at::kByte, *x);
+    const Ref rows = args[4] != Py_None || format != BWLA_FP4_NV ? Ref(Py_NewRef(args[4])) : fp4_new({M}, at::kFloat, *x);
+    if (!codes.o || !scales.o || !rows.o || !fp4_rows(codes.o, scales.o, rows.o, format, names, &q)) return nullptr;
+    if (q.rows != M || q.K != K / 2 * 2) { PyErr_SetString(PyExc_TypeError, "codes must be [M][K/2] for x of [M][K]"); return nullptr; }
+    return fp4_result(unlocked(entry.fp4_quantize, (const void*)x->data_ptr(), float_dtype(*x), M, K, M > 0 ? x->stride(0) : K, format, (uint8_t*)q.codes,
+                               (uint8_t*)q.scales, (float*)q.row_scales, stream()),
+                      PyTuple_Pack(3, codes.o, scales.o, rows.o));
     END_HANDLE_TH_ERRORS
 }
 
-// fp4_expand(codes, scales, row_scales, format, out) -> status
+// fp4_expand(codes, scales, row_scales, format, out) -> out, or status; out: a tensor, or 0 (bf16) or 1 (fp32) for a new one
 PyObject* call_fp4_expand(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
     if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "fp4_expand(codes, scales, row_scales, format, out)"); return nullptr; }
     static const char* names[3] = {"codes", "scales", "row_scales"};
     int format;
     Fp4Rows q;
-    const at::Tensor* out = tensor(args[4], "out");
-    if (!out || !fp4_format(args[3], &format) || !fp4_rows(args[0], args[1], args[2], format, names, &q)) return nullptr;
+    if (!fp4_format(args[3], &format) || !fp4_rows(args[0], args[1], args[2], format, names, &q)) return nullptr;
+    const Ref made = PyLong_Check(args[4]) ? fp4_new({q.rows, q.K}, PyLong_AsLong(args[4]) ? at::kFloat : at::kBFloat16, THPVariable_Unpack(args[0])) : Ref(Py_NewRef(args[4]));
+    const at::Tensor* out = made.o ? tensor(made.o, "out") : nullptr;
+    if (!out) return nullptr;
     if (float_dtype(*out) != BWLA_DTYPE_F32 && float_dtype(*out) != BWLA_DTYPE_BF16) { PyErr_SetString(PyExc_TypeError, "out must be fp32 or bf16"); return nullptr; }
-    if (!need(args[4], out->scalar_type(), "out", 2) || !here(*out, "out")) return nullptr;
+    if (!need(made.o, out->scalar_type(), "out", 2) || !here(*out, "out")) return nullptr;
     if (out->size(0) != q.rows || out->size(1) != q.K) { PyErr_SetString(PyExc_TypeError, "out must be [M][K] for codes of [M][K/2]"); return nullptr; }
-    return unlocked(entry.fp4_expand, (const uint8_t*)q.codes, (const uint8_t*)q.scales, (const float*)q.row_scales, q.rows, q.K, format, out->data_ptr(),
-                    float_dtype(*out), q.rows > 0 ? out->stride(0) : q.K, stream());
+    return fp4_result(unlocked(entry.fp4_expand, (const uint8_t*)q.codes, (const uint8_t*)q.scales, (const float*)q.row_scales, q.rows, q.K, format,
+                               out->data_ptr(), float_dtype(*out), q.rows > 0 ? out->stride(0) : q.K, stream()),
+                      Py_NewRef(made.o));
     END_HANDLE_TH_ERRORS
 }
 
-// fp4_gemm(a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, format, out, workspace) -> status
+// fp4_gemm(a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, format, out, workspace) -> out (made here where it is None), or status
 PyObject* call_fp4_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
     if (nargs != 9) { PyErr_SetString(PyExc_TypeError, "fp4_gemm: nine arguments"); return nullptr; }
@@ -262,36 +281,40 @@ PyObject* call_fp4_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     int format;
     Fp4Rows a, w;
     const at::Tensor *out, *ws;
-    if (!fp4_format(args[6], &format) || !fp4_rows(args[0], args[1], args[2], format, a_names, &a) || !fp4_rows(args[3], args[4], args[5], format, w_names, &w) ||
-        !(out = need(args[7], at::kBFloat16, "out", 2)) || !here(*out, "out") || !(ws = tensor(args[8], "workspace")) || !here(*ws, "workspace"))
+    if (!fp4_format(args[6], &format) || !fp4_rows(args[0], args[1], args[2], format, a_names, &a) || !fp4_rows(args[3], args[4], args[5], format, w_names, &w))
+        return nullptr;
+    const Ref made = args[7] != Py_None ? Ref(Py_NewRef(args[7])) : fp4_new({a.rows, w.rows}, at::kBFloat16, THPVariable_Unpack(args[0]));
+    if (!made.o || !(out = need(made.o, at::kBFloat16, "out", 2)) || !here(*out, "out") || !(ws = tensor(args[8], "workspace")) || !here(*ws, "workspace"))
         return nullptr;
     if (a.K != w.K || out->size(0) != a.rows || out->size(1) != w.rows) {
         PyErr_SetString(PyExc_TypeError, "a_codes [M][K/2], w_codes [N][K/2] and out [M][N] do not fit");
         return nullptr;
     }
-    return unlocked(entry.fp4_gemm, (const uint8_t*)a.codes, (const uint8_t*)a.scales, (const float*)a.row_scales, a.rows, a.K, (const uint8_t*)w.codes,
-                    (const uint8_t*)w.scales, (const float*)w.row_scales, w.rows, format, out->data_ptr(), a.rows > 0 ? out->stride(0) : w.rows, ws->data_ptr(),
-                    (size_t)ws->nbytes(), stream());
+    return fp4_result(unlocked(entry.fp4_gemm, (const uint8_t*)a.codes, (const uint8_t*)a.scales, (const float*)a.row_scales, a.rows, a.K, (const uint8_t*)w.codes,
+                               (const uint8_t*)w.scales, (const float*)w.row_scales, w.rows, format, out->data_ptr(), a.rows > 0 ? out->stride(0) : w.rows,
+                               ws->data_ptr(), (size_t)ws->nbytes(), stream()),
+                      Py_NewRef(made.o));
     END_HANDLE_TH_ERRORS
 }
 
-// fp4_linear(layer, x, out, workspace) -> status
+// fp4_linear(layer, x, out, workspace) -> out (made here where it is None), or status
 PyObject* call_fp4_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
     if (nargs != 4) { PyErr_SetString(PyExc_TypeError, "fp4_linear(layer, x, out, workspace)"); return nullptr; }
     const at::Tensor *x = need(args[1], at::kBFloat16, "x", 2), *out, *ws;
-    if (!x || !here(*x, "x") || !(out = need(args[2], at::kBFloat16, "out", 2)) || !here(*out, "out") || !(ws = tensor(args[3], "workspace")) || !here(*ws, "workspace"))
-        return nullptr;
-    PyObject* o = PyObject_GetAttr(args[0], name_fp4);
-    if (!o) return nullptr;
-    Ref h(o);
-    const bwla_fp4_layer* layer = o == Py_None ? nullptr : (const bwla_fp4_layer*)PyLong_AsVoidPtr(o);
+    if (!x || !here(*x, "x") || !(ws = tensor(args[3], "workspace")) || !here(*ws, "workspace")) return nullptr;
+    const Ref h(PyObject_GetAttr(args[0], name_fp4));
+    if (!h.o) return nullptr;
+    const bwla_fp4_layer* layer = h.o == Py_None ? nullptr : (const bwla_fp4_layer*)PyLong_AsVoidPtr(h.o);
     int64_t K, N;
     if (PyErr_Occurred() || !size_of(args[0], name_k, &K) || !size_of(args[0], name_n, &N)) return nullptr;
     const int64_t M = x->size(0);
+    const Ref made = args[2] != Py_None ? Ref(Py_NewRef(args[2])) : fp4_new({M, N}, at::kBFloat16, *x);
+    if (!made.o || !(out = need(made.o, at::kBFloat16, "out", 2)) || !here(*out, "out")) return nullptr;
     if (x->size(1) != K || out->size(0) != M || out->size(1) != N) { PyErr_SetString(PyExc_TypeError, "x must be [M][K] and out [M][N] of the layer"); return nullptr; }
-    return unlocked(entry.fp4_linear, layer, (const void*)x->data_ptr(), M, M > 0 ? x->stride(0) : K, out->data_ptr(), M > 0 ? out->stride(0) : N, ws->data_ptr(),
-                    (size_t)ws->nbytes(), stream());
+    return fp4_result(unlocked(entry.fp4_linear, layer, (const void*)x->data_ptr(), M, M > 0 ? x->stride(0) : K, out->data_ptr(), M > 0 ? out->stride(0) : N,
+                               ws->data_ptr(), (size_t)ws->nbytes(), stream()),
+                      Py_NewRef(made.o));
     END_HANDLE_TH_ERRORS
 }
 
