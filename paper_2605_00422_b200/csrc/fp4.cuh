@@ -109,22 +109,42 @@ __device__ __forceinline__ Fp4Block fp4_block_mx(float top) {
     b.mul = finite ? fp4_pow2(-e) : 0.f;
     return b;
 }
-// to_row: 2^-E of the row
+// to_row: 2^-E of the row.  EXACT: top has 24 bits, else up to 11.  (1/6 in fp32 is above 1/6 by half of 2^-24 of it; see fp4_divide8.)
+template <bool EXACT>
 __device__ __forceinline__ Fp4Block fp4_block_nv(float top, float to_row) {
     Fp4Block b;
-    const uint32_t byte = fp4_e4m3(fp4_quotient(__fmul_rn(top, to_row), 6.f, 1.f / 6.f));
+    const float t = __fmul_rn(top, to_row);
+    const uint32_t byte = fp4_e4m3(EXACT ? fp4_quotient(t, 6.f, 1.f / 6.f) : __fmul_rz(t, 1.f / 6.f));
     b.byte = top == 0.f ? 0u : max(byte, 1u);
     b.div = fp4_from_e4m3(b.byte);
-    b.inv = b.byte ? __frcp_rn(b.div) : 0.f;
+    // the reciprocal of a number of four bits to nearest: the hardware's estimate and one Newton step
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(b.div));
+    r = __fmaf_rn(__fmaf_rn(-b.div, r, 1.f), r, r);
+    b.inv = b.byte ? r : 0.f;
     return b;
 }
-// One value's quotient by its block's scale, for the rounding to e2m1.  EXACT: for values of up to 24 bits; those of up to 11 (bf16,
-// fp16) miss the middle between two codes, a number of 7 bits in units of the scale, by 2^-11 of it or not at all, so rounding the product
-// to 16 bits decides alike.
+
+// Eight values by their block's scale, for the rounding to e2m1; mul: 1 / (scale * 2^E).
+// A code is decided against the middles T between codes, numbers of up to three bits, and 1 / scale, rounded, is never below the exact
+// one: the scale has four bits, and 1/9 to 1/15 are all rounded up in fp32, by less than 2^-24 of themselves.  So where the quotient is
+// T the product rounded towards zero is T.  Values of up to 11 bits (bf16, fp16) otherwise miss T by 2^-11 of it, and the product is all there
+// is to do.  EXACT, for values of 24 bits: products within four units of a T are divided with the residual instead.
 template <bool EXACT>
-__device__ __forceinline__ float fp4_divide(float x, const Fp4Block& b) {
-    if (EXACT) return fp4_quotient(x, b.div, b.inv);
-    return __uint_as_float((__float_as_uint(__fmul_rn(x, b.inv)) + 0x80u) & 0xFFFFFF00u);
+__device__ __forceinline__ void fp4_divide8(float (&f)[8], const Fp4Block& b, float mul, float to_row) {
+    float q[8];
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        q[i] = __fmul_rz(f[i], mul);
+        if (EXACT) near = near || ((__float_as_uint(q[i]) + 4u) & 0x1FFFF8u) == 0u;
+    }
+    if (EXACT && near) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = fp4_quotient(__fmul_rn(f[i], to_row), b.div, b.inv);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = q[i];
 }
 
 int launch_fp4_quantize(const void* x, int dtype, int64_t M, int64_t K, int64_t ldx, int format, uint8_t* codes, uint8_t* scales, float* row_scales,

@@ -5,9 +5,11 @@
 //   NV   2^E from the row's largest magnitude, s = e4m3(top / (6 2^E)) (at least 2^-9), code = e2m1(x / (s 2^E))
 // A block (MX) or a row (NV) with an infinity or a NaN stands for NaN throughout: byte 255, or a NaN row scale; its codes are zeros.
 //
-// Bound by memory: 2 or 4 bytes a value in, a half and a scale's share out.  A thread takes 8 neighbouring values (one 16-byte load of a
-// 16-bit type), 4 threads a block of 32, 2 one of 16; their maxima meet by shuffles.  The threads of a row (32, 128 or 512, so that a
-// thread has up to kHold pieces) keep what they have read in registers, so the row maximum of NV costs no second pass over memory.
+// Bound by memory: 2 or 4 bytes a value in, a half and a scale's share out, if a value takes no more than some 14 instructions (16-bit types).
+// A thread takes pieces of 16 neighbouring values, a block of NV or half of one of MX (the halves' maxima meet by a shuffle): with 8 a thread,
+// the block's scale worked out by two or four threads, NV took 24 instructions a value and 19.2 us for 4096 x 5120 bf16.  A row has a warp (up
+// to 1024 values) or a block of as many threads as leave each a few pieces, which it keeps in registers: the row maximum of NV costs no second
+// pass over memory.
 #include "fp4.cuh"
 #include "umma_ptx.cuh"
 
@@ -15,44 +17,40 @@ namespace bwla {
 
 using namespace ptx;
 
-namespace fp4_rows {
-constexpr int kThreads = 512;
-constexpr int kHold = 8;                 // pieces of 8 values a thread keeps
-}  // namespace fp4_rows
+constexpr int kPiece = 16;                // values
 
-template <typename T> struct RawPiece { uint4 v; };
-template <> struct RawPiece<float> { uint4 v, w; };
+template <typename T> struct RawPiece { uint4 v[sizeof(T)]; };      // 32 or 64 bytes
 
 template <typename T>
 __device__ __forceinline__ RawPiece<T> load_piece(const T* p, bool vec) {
     RawPiece<T> r;
     if (vec) {
-        r.v = __ldg(reinterpret_cast<const uint4*>(p));
-        if constexpr (sizeof(T) == 4) r.w = __ldg(reinterpret_cast<const uint4*>(p) + 1);
-    } else {
-        uint32_t u[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(p[i]);
-            else u[i] = reinterpret_cast<const uint16_t*>(p)[i];
-        }
-        if constexpr (sizeof(T) == 4) {
-            r.v = make_uint4(u[0], u[1], u[2], u[3]);
-            r.w = make_uint4(u[4], u[5], u[6], u[7]);
-        } else {
-            r.v = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
+        for (int i = 0; i < (int)sizeof(T); ++i) r.v[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); ++i) {
+            if constexpr (sizeof(T) == 4) {
+                r.v[i] = make_uint4(__float_as_uint(p[4 * i]), __float_as_uint(p[4 * i + 1]), __float_as_uint(p[4 * i + 2]), __float_as_uint(p[4 * i + 3]));
+            } else {
+                const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + 8 * i;
+                r.v[i] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+            }
         }
     }
     return r;
 }
+// values 8 half .. 8 half + 7
 template <typename T>
-__device__ __forceinline__ void piece_values(const RawPiece<T>& r, float (&f)[8]) {
-    const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
+__device__ __forceinline__ void piece_values(const RawPiece<T>& r, int half, float (&f)[8]) {
     if constexpr (sizeof(T) == 4) {
-        const uint32_t w2[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+        const uint4 a = r.v[2 * half], b = r.v[2 * half + 1];
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[i] = __uint_as_float(w[i]); f[4 + i] = __uint_as_float(w2[i]); }
+        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
     } else {
+        const uint4 a = r.v[half];
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (std::is_same<T, __nv_bfloat16>::value) {
@@ -66,12 +64,24 @@ __device__ __forceinline__ void piece_values(const RawPiece<T>& r, float (&f)[8]
         }
     }
 }
-// bits of the largest magnitude (an infinity or a NaN is larger than every number)
-__device__ __forceinline__ uint32_t top_bits(const float (&f)[8]) {
+// Bits of the largest magnitude as fp32 (an infinity or a NaN is larger than every number).  Magnitudes order like their bit patterns, those of
+// 16-bit types two at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t top_bits(const RawPiece<T>& r) {
     uint32_t t = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t = max(t, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-    return t;
+    for (int i = 0; i < (int)sizeof(T); ++i) {
+        const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 4) t = max(t, w[j] & 0x7FFFFFFFu);
+            else asm("max.s16x2 %0, %0, %1;" : "+r"(t) : "r"(w[j] & 0x7FFF7FFFu));
+        }
+    }
+    if constexpr (sizeof(T) == 4) return t;
+    const uint32_t h = max(t >> 16, t & 0xFFFFu);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) return h << 16;
+    else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)h)));
 }
 
 struct Fp4QuantParams {
@@ -81,83 +91,89 @@ struct Fp4QuantParams {
     uint8_t* codes; uint8_t* scales; float* row_scales;
 };
 
-// G threads a row.  HOLD: a thread keeps its pieces (K <= 8 G kHold), else they are read again behind the row maximum.
-template <typename T, bool NV, int G, bool HOLD>
-__global__ void __launch_bounds__(fp4_rows::kThreads) fp4_quantize_kernel(const Fp4QuantParams p) {
-    using namespace fp4_rows;
-    constexpr int kRows = kThreads / G, kWarps = G / 32;
-    __shared__ uint32_t red[kRows][kWarps > 1 ? kWarps : 1];
-    const int sub = threadIdx.x / G, tid = threadIdx.x % G, lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * kRows + sub;
+// P: pieces a thread keeps; 0: any number, read again behind the row maximum.  ROWS: rows a block (a warp each), or 1.
+template <typename T, bool NV, int P, int ROWS>
+__global__ void __launch_bounds__(ROWS > 1 ? 32 * ROWS : 1024) fp4_quantize_kernel(const Fp4QuantParams p) {
+    __shared__ uint32_t red[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tid = ROWS > 1 ? lane : (int)(NV ? threadIdx.x : blockIdx.y * blockDim.x + threadIdx.x), G = ROWS > 1 ? 32 : (int)blockDim.x;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? warp : 0);
     const bool live = row < p.M;
-    const int pieces = (int)(p.K >> 3);
+    const int pieces = (int)(p.K >> 4);
+    const int full = (int)p.col_tiles * (NV ? 4 : 8);      // with the blocks that fill the last tile (scales: zeros, codes: none)
     const T* x = reinterpret_cast<const T*>(p.x) + (live ? row : 0) * p.ldx;
+    uint2* const codes = reinterpret_cast<uint2*>(p.codes) + row * pieces;
+    uint8_t* const scales = p.scales + fp4_scale_at(row, 0, p.col_tiles);
+    const bool vec = p.vec != 0;
     griddep_wait();
     if (p.chained) griddep_launch_dependents();
-    RawPiece<T> held[HOLD ? kHold : 1];
-    if (HOLD) {
+    auto load = [&](int c) {
+        RawPiece<T> r;
 #pragma unroll
-        for (int i = 0; i < kHold; ++i) {
-            const int c = tid + i * G;
-            held[i].v = make_uint4(0u, 0u, 0u, 0u);
-            if constexpr (sizeof(T) == 4) held[i].w = make_uint4(0u, 0u, 0u, 0u);
-            if (live && c < pieces) held[i] = load_piece(x + (size_t)c * 8, p.vec != 0);
-        }
-    }
+        for (int i = 0; i < (int)sizeof(T); ++i) r.v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (live && c < pieces) r = load_piece(x + (size_t)c * kPiece, vec);
+        return r;
+    };
+    RawPiece<T> held[P > 0 ? P : 1];
+#pragma unroll
+    for (int i = 0; i < P; ++i) held[i] = load(tid + i * G);
     float to_row = 1.f;                      // 2^-E
-    bool bad = false;
+    bool bad = false, tiny = false;
     if (NV) {
         uint32_t top = 0u;
-        if (HOLD) {
+        if (P > 0) {
 #pragma unroll
-            for (int i = 0; i < kHold; ++i) { float f[8]; piece_values(held[i], f); top = max(top, top_bits(f)); }
+            for (int i = 0; i < P; ++i) top = max(top, top_bits(held[i]));
         } else {
-            for (int c = tid; live && c < pieces; c += G) { float f[8]; piece_values(load_piece(x + (size_t)c * 8, p.vec != 0), f); top = max(top, top_bits(f)); }
+            for (int c = tid; c < pieces; c += G) top = max(top, top_bits(load(c)));
         }
         top = __reduce_max_sync(0xFFFFFFFFu, top);
-        if (kWarps > 1) {
-            if (lane == 0) red[sub][tid >> 5] = top;
+        if (ROWS == 1) {
+            if (lane == 0) red[warp] = top;
             __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = max(top, red[sub][w]);
+            top = __reduce_max_sync(0xFFFFFFFFu, lane < (int)(blockDim.x >> 5) ? red[lane] : 0u);
         }
         bad = top >= 0x7F800000u;
         const int E = bad ? 0 : fp4_row_exponent(__uint_as_float(top));
         to_row = fp4_pow2(-E);
+        tiny = E < -100;                     // 1 / scale times 2^-E might not be a number: the rows are scaled first
         if (live && tid == 0) p.row_scales[row] = bad ? __int_as_float(0x7FC00000) : fp4_pow2(E);
     }
-    const int full = (int)p.col_tiles * 4 * (NV ? 2 : 4);      // pieces with the blocks that fill the last tile (codes: none)
     auto put = [&](int c, const RawPiece<T>& raw) {
-        float f[8];
-        piece_values(raw, f);
-        uint32_t top = top_bits(f);
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        if (!NV) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        uint32_t top = top_bits(raw);
+        if (!NV) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        uint32_t word[2];
         Fp4Block b;
-        if (NV) {
-            b = fp4_block_nv(bad ? 0.f : __uint_as_float(top), to_row);
-            // (in units of the row's scale: exact, but for values far below the smallest code)
+        if (NV) b = fp4_block_nv<sizeof(T) == 4>(bad ? 0.f : __uint_as_float(top), to_row);
+        else b = fp4_block_mx(__uint_as_float(top));
+        const float mul = NV ? __fmul_rn(b.inv, tiny ? 1.f : to_row) : b.mul;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = bad ? 0.f : fp4_divide<sizeof(T) == 4>(__fmul_rn(f[i], to_row), b);
-        } else {
-            b = fp4_block_mx(__uint_as_float(top));
-            const bool nan = b.byte == 255u;
+        for (int h = 0; h < 2; ++h) {
+            float f[8];
+            piece_values(raw, h, f);
+            if (NV) {
+                if (tiny) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = nan ? 0.f : __fmul_rn(f[i], b.mul);
+                    for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(f[i], to_row);
+                }
+                fp4_divide8<sizeof(T) == 4>(f, b, mul, tiny ? 1.f : to_row);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(f[i], mul);
+            }
+            word[h] = fp4_codes8(f);
         }
-        const uint32_t codes = fp4_codes8(f);
-        if (live && c < pieces) reinterpret_cast<uint32_t*>(p.codes)[(size_t)row * pieces + c] = codes;
-        if (live && c < full && (c & (NV ? 1 : 3)) == 0) p.scales[fp4_scale_at(row, c >> (NV ? 1 : 2), p.col_tiles)] = (uint8_t)(c < pieces ? b.byte : 0u);
+        if (NV ? bad : b.byte == 255u) word[0] = word[1] = 0u;
+        const int j = NV ? c : c >> 1;                          // block
+        if (live && c < pieces) codes[c] = make_uint2(word[0], word[1]);
+        if (live && c < full && (NV || (c & 1) == 0)) scales[(size_t)(j >> 2) * 512 + (j & 3)] = (uint8_t)(c < pieces ? b.byte : 0u);
     };
-    if (HOLD) {
+    if (P > 0) {
 #pragma unroll
-        for (int i = 0; i < kHold; ++i)
+        for (int i = 0; i < P; ++i)
             if (i * G < full) put(tid + i * G, held[i]);
     } else {
-        RawPiece<T> none;
-        none.v = make_uint4(0u, 0u, 0u, 0u);
-        if constexpr (sizeof(T) == 4) none.w = none.v;
-        for (int c = tid; c - tid < full; c += G) put(c, live && c < pieces ? load_piece(x + (size_t)c * 8, p.vec != 0) : none);
+        for (int c = tid; c - tid < full; c += G) put(c, load(c));
     }
     // (a kernel behind this one that does not wait for it, because what it reads first are constants to it, starts when all blocks have ended)
     if (!p.chained) __threadfence();
@@ -165,14 +181,25 @@ __global__ void __launch_bounds__(fp4_rows::kThreads) fp4_quantize_kernel(const 
 
 template <typename T, bool NV>
 static int quantize_rows(const Fp4QuantParams& p, cudaStream_t stream) {
-    using namespace fp4_rows;
-    const int64_t per = 8 * kHold;
-    void (*k)(Fp4QuantParams) = p.K <= 32 * per ? fp4_quantize_kernel<T, NV, 32, true> : p.K <= 128 * per ? fp4_quantize_kernel<T, NV, 128, true>
-                              : p.K <= 512 * per ? fp4_quantize_kernel<T, NV, 512, true> : fp4_quantize_kernel<T, NV, 512, false>;
-    const int rows = p.K <= 32 * per ? kThreads / 32 : p.K <= 128 * per ? kThreads / 128 : 1;
+    constexpr int kMost = sizeof(T) == 4 ? 2 : 4;               // (1024 threads of 64 registers hold no more)
+    const int64_t full = p.col_tiles * (NV ? 4 : 8);
+    void (*k)(Fp4QuantParams);
+    int rows = 1, threads = 1024;
+    int64_t parts = 1;
+    if (full <= 64) {
+        rows = 8; threads = 256;
+        k = full <= 32 ? fp4_quantize_kernel<T, NV, 1, 8> : fp4_quantize_kernel<T, NV, 2, 8>;
+    } else {
+        // (blocks of MX are independent: a row in parts)
+        const int per = !NV || full <= 512 ? 1 : full <= 1024 ? 2 : full <= 1024 * kMost ? kMost : 0;
+        if (!NV) parts = (full + 511) / 512;
+        if (per) threads = (int)((full + 32 * per * parts - 1) / (32 * per * parts) * 32);
+        k = !NV ? fp4_quantize_kernel<T, NV, 1, 1> : per == 1 ? fp4_quantize_kernel<T, NV, 1, 1> : per == 2 ? fp4_quantize_kernel<T, NV, NV ? 2 : 1, 1> : per ? fp4_quantize_kernel<T, NV, NV ? kMost : 1, 1>
+                                                                                               : fp4_quantize_kernel<T, NV, NV ? 0 : 1, 1>;
+    }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((p.M + rows - 1) / rows), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.gridDim = dim3((unsigned)((p.M + rows - 1) / rows), (unsigned)parts, 1);
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -210,24 +237,16 @@ struct Fp4ExpandParams {
 };
 
 template <typename T, bool NV>
-__global__ void __launch_bounds__(256) fp4_expand_kernel(const Fp4ExpandParams p) {
-    const int pieces = (int)(p.K >> 3);
-    const int per_block = (pieces + 255) / 256;
-    const int64_t row = (int64_t)blockIdx.x / per_block;
-    const int c = (int)((int64_t)blockIdx.x - row * per_block) * 256 + threadIdx.x;
-    griddep_wait();
-    if (c >= pieces) return;
+__device__ __forceinline__ void expand_piece(T* out, uint32_t codes, uint32_t byte, float r, bool vec) {
     float v[8];
-    fp4_values8(__ldg(reinterpret_cast<const uint32_t*>(p.codes) + (size_t)row * pieces + c), v);
-    const float s = fp4_block_scale<NV>(__ldg(p.scales + fp4_scale_at(row, c >> (NV ? 1 : 2), p.col_tiles)));
-    const float r = p.row_scales ? __ldg(p.row_scales + row) : 1.f;
+    fp4_values8(codes, v);
+    const float s = fp4_block_scale<NV>(byte);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(__fmul_rn(v[i], s), r);
-    T* out = reinterpret_cast<T*>(p.out) + (size_t)row * p.ldo + (size_t)c * 8;
     if constexpr (sizeof(T) == 4) {
-        if (p.vec) {
-            reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        if (vec) {
+            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"       // (a whole sector)
+                         ::"l"(out), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) out[i] = v[i];
@@ -236,7 +255,7 @@ __global__ void __launch_bounds__(256) fp4_expand_kernel(const Fp4ExpandParams p
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
-        if (p.vec) {
+        if (vec) {
             *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
 #pragma unroll
@@ -245,19 +264,43 @@ __global__ void __launch_bounds__(256) fp4_expand_kernel(const Fp4ExpandParams p
     }
 }
 
-int launch_fp4_expand(const uint8_t* codes, const uint8_t* scales, const float* row_scales, int64_t M, int64_t K, int format, void* out, int dtype,
-                      int64_t ldo, cudaStream_t stream) {
-    Fp4ExpandParams p{};
-    p.codes = codes; p.scales = scales; p.row_scales = row_scales; p.M = M; p.K = K; p.col_tiles = fp4_col_tiles(K, format); p.out = out; p.ldo = ldo;
-    p.vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ldo % (dtype == BWLA_DTYPE_F32 ? 4 : 8) == 0;
-    const int64_t blocks = M * ((K / 8 + 255) / 256);
-    if (blocks >= ((int64_t)1 << 31)) return BWLA_ERR_INVALID_ARG;
-    const bool nv = format == BWLA_FP4_NV;
-    void (*k)(Fp4ExpandParams) = dtype == BWLA_DTYPE_F32 ? (nv ? fp4_expand_kernel<float, true> : fp4_expand_kernel<float, false>)
-                                                         : (nv ? fp4_expand_kernel<__nv_bfloat16, true> : fp4_expand_kernel<__nv_bfloat16, false>);
+// A thread takes two pieces of 8 values, ROWS rows a block a warp each (short rows), or a part of one row a block; rows beyond the grid's second
+// dimension in turn.
+template <typename T, bool NV, int ROWS>
+__global__ void __launch_bounds__(ROWS > 1 ? 32 * ROWS : 512) fp4_expand_kernel(const Fp4ExpandParams p) {
+    const int pieces = (int)(p.K >> 3);
+    const int step = ROWS > 1 ? 32 : (int)blockDim.x;
+    const int c0 = ROWS > 1 ? (int)(threadIdx.x & 31) : (int)(blockIdx.x * 2 * blockDim.x + threadIdx.x);
+    griddep_wait();
+    for (int64_t row = (int64_t)blockIdx.y * ROWS + (ROWS > 1 ? threadIdx.x >> 5 : 0); row < p.M; row += (int64_t)gridDim.y * ROWS) {
+        const uint32_t* codes = reinterpret_cast<const uint32_t*>(p.codes) + row * pieces;
+        const uint8_t* scales = p.scales + fp4_scale_at(row, 0, p.col_tiles);
+        const float r = p.row_scales ? __ldg(p.row_scales + row) : 1.f;
+        T* out = reinterpret_cast<T*>(p.out) + (size_t)row * p.ldo;
+        uint32_t word[2], byte[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int c = c0 + u * step, j = c >> (NV ? 1 : 2);
+            word[u] = c < pieces ? __ldg(codes + c) : 0u;
+            byte[u] = c < pieces ? __ldg(scales + (size_t)(j >> 2) * 512 + (j & 3)) : 0u;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int c = c0 + u * step;
+            if (c < pieces) expand_piece<T, NV>(out + (size_t)c * 8, word[u], byte[u], r, p.vec != 0);
+        }
+    }
+}
+
+template <typename T, bool NV>
+static int expand_rows(const Fp4ExpandParams& p, cudaStream_t stream) {
+    const int64_t pieces = p.K / 8;
+    const bool several = pieces <= 64;
+    const int64_t parts = (pieces + 1023) / 1024;
+    const int threads = several ? 256 : (int)(((pieces + 2 * parts - 1) / (2 * parts) + 31) / 32 * 32);
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)blocks, 1, 1);
-    cfg.blockDim = dim3(256, 1, 1);
+    cfg.gridDim = dim3(several ? 1u : (unsigned)parts, (unsigned)std::min<int64_t>(several ? (p.M + 7) / 8 : p.M, 65535), 1);
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -265,9 +308,19 @@ int launch_fp4_expand(const uint8_t* codes, const uint8_t* scales, const float* 
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     ProfScope prof(kProfPrepare, stream);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, several ? fp4_expand_kernel<T, NV, 8> : fp4_expand_kernel<T, NV, 1>, p);
     if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e); }
     return after_launch();
+}
+
+int launch_fp4_expand(const uint8_t* codes, const uint8_t* scales, const float* row_scales, int64_t M, int64_t K, int format, void* out, int dtype,
+                      int64_t ldo, cudaStream_t stream) {
+    Fp4ExpandParams p{};
+    p.codes = codes; p.scales = scales; p.row_scales = row_scales; p.M = M; p.K = K; p.col_tiles = fp4_col_tiles(K, format); p.out = out; p.ldo = ldo;
+    p.vec = (reinterpret_cast<uintptr_t>(out) & (dtype == BWLA_DTYPE_F32 ? 31 : 15)) == 0 && ldo % 8 == 0;
+    const bool nv = format == BWLA_FP4_NV;
+    if (dtype == BWLA_DTYPE_F32) return nv ? expand_rows<float, true>(p, stream) : expand_rows<float, false>(p, stream);
+    return nv ? expand_rows<__nv_bfloat16, true>(p, stream) : expand_rows<__nv_bfloat16, false>(p, stream);
 }
 
 }  // namespace bwla
