@@ -307,9 +307,9 @@ int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const f
  * full scale); a code or block scale can differ from the exact Y's only where that decides.
  *   x_bf16 device, bf16 [M][ldx]; P1, P2 as for bwla_rotate_quant_act.  Factor sizes the tensor-core rotation does not take
  *   (n2 % 8 != 0, n2 > 256, n1 > 192) return BWLA_ERR_UNSUPPORTED.
- *   workspace of bwla_rotate_quant_fp4_workspace_bytes, its first 256 bytes as above
+ *   workspace of bwla_rotate_quant_fp4_workspace_bytes (0 for factor sizes that are not taken), its first 256 bytes as above
  */
-size_t bwla_rotate_quant_fp4_workspace_bytes(int64_t M, int64_t K);
+size_t bwla_rotate_quant_fp4_workspace_bytes(int64_t M, int64_t K, int n1, int n2);
 int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const float* P1, int n1, const float* P2, int n2,
                           int format, uint8_t* codes, uint8_t* scales, float* row_scales, void* workspace, size_t workspace_bytes,
                           void* stream);

@@ -98,7 +98,7 @@ def _load() -> C.CDLL:
     lib.bwla_fp4_expand_rows.argtypes = [vp, vp, vp, i64, i64, ci, vp, ci, i64, vp]
     lib.bwla_fp4_gemm_workspace_bytes.argtypes = [i64, i64, i64]
     lib.bwla_fp4_gemm_codes.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp, i64, ci, vp, i64, vp, sz, vp]
-    lib.bwla_rotate_quant_fp4_workspace_bytes.argtypes = [i64, i64]
+    lib.bwla_rotate_quant_fp4_workspace_bytes.argtypes = [i64, i64, ci, ci]
     lib.bwla_rotate_quant_fp4.argtypes = [vp, i64, i64, i64, vp, ci, vp, ci, ci, vp, vp, vp, vp, sz, vp]
     lib.bwla_fp4_layer_prepared_bytes.argtypes = [i64, ci, ci]
     lib.bwla_fp4_layer_create.argtypes = [C.POINTER(vp), i64, i64, vp, ci, vp, ci, ci, vp, vp, vp, vp, sz, vp]
@@ -482,8 +482,8 @@ def bwla_fp4_gemm_codes(a_codes: torch.Tensor, a_scales: torch.Tensor, a_rows: O
     return made
 
 
-def bwla_rotate_quant_fp4_workspace_bytes(M: int, K: int) -> int:
-    return int(_lib.bwla_rotate_quant_fp4_workspace_bytes(M, K))
+def bwla_rotate_quant_fp4_workspace_bytes(M: int, K: int, n1: int, n2: int) -> int:
+    return int(_lib.bwla_rotate_quant_fp4_workspace_bytes(M, K, n1, n2))
 
 
 def bwla_rotate_quant_fp4(x: torch.Tensor, P1: torch.Tensor, P2: torch.Tensor, format: int, workspace: Optional[torch.Tensor] = None):
@@ -495,7 +495,7 @@ def bwla_rotate_quant_fp4(x: torch.Tensor, P1: torch.Tensor, P2: torch.Tensor, f
         raise TypeError("P1 and P2 must be contiguous")
     M, K = x.shape
     if workspace is None:
-        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, K)), dtype=torch.uint8, device=x.device)
+        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, K, P1.shape[0], P2.shape[0])), dtype=torch.uint8, device=x.device)
     codes, scales, rows = _fp4_outputs(M, K, format, x.device)
     st = _lib.bwla_rotate_quant_fp4(_ptr(x), M, K, x.stride(0) if M > 0 else K, _ptr(P1), P1.shape[0], _ptr(P2), P2.shape[0], format, _ptr(codes),
                                     _ptr(scales), _ptr(rows), _ptr(workspace), workspace.numel(), _stream())
@@ -558,7 +558,7 @@ def bwla_fp4_layer_rotate_quant(layer: Fp4Layer, x: torch.Tensor, workspace: Opt
     if x.shape[1] != layer.K:
         raise TypeError("x must be [M][K] of the layer")
     if workspace is None:
-        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, layer.K)), dtype=torch.uint8, device=x.device)
+        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, layer.K, layer.n1, layer.n2)), dtype=torch.uint8, device=x.device)
     codes, scales, rows = _fp4_outputs(M, layer.K, layer.format, x.device)
     st = _lib.bwla_fp4_layer_rotate_quant(layer.handle, _ptr(x), M, x.stride(0) if M > 0 else layer.K, _ptr(codes), _ptr(scales), _ptr(rows),
                                           _ptr(workspace), workspace.numel(), _stream())

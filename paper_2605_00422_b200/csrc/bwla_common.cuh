@@ -156,6 +156,10 @@ struct RotProblem {
     float* ysum;                // [M] sums of the rounded values, or NULL
     // final binarisation
     uint32_t* packed; float *alpha, *mu;
+    // microscaled 4-bit codes (fp4.cuh): 1 MX, 2 NV; hold: no dependent kernel starts before this one has ended, because one may read the
+    // outputs without waiting
+    int fp4, hold;
+    uint8_t *fp4_codes, *fp4_scales; float* fp4_rows;
 };
 // V == NULL: no T = V x.  lr_part, lr_count: of the blocks beside the rotation; umma_part: of lowrank_umma.cu, may overlap the codes.
 struct OktLowrank { const void* V; int r; void* Thl; float* lr_part; uint32_t* lr_count; float* umma_part; };
@@ -170,6 +174,8 @@ int launch_prepare_rot(const RotGeom& g, const float* P1, const float* P2, void*
 // behind: SMs that the kernel behind it takes at once (0: not known; only asked for with raw factors and few tokens).
 int launch_rot(const RotGeom& g, const void* x, int64_t M, int64_t ldx, int bits, int asym, int n_problems,
                const RotProblem* problems, const OktLowrank* lowrank, uint32_t* status, cudaStream_t stream, int behind = 0);
+// One linear's microscaled 4-bit codes, by the kernel that launch_rot would take where that writes them (*taken; else nothing has been launched).
+int launch_rot_fp4(const RotGeom& g, const void* x, int64_t M, int64_t ldx, const RotProblem& problem, uint32_t* status, bool* taken, cudaStream_t stream);
 // The same for many tokens, on the tcgen05 tensor cores (rot_umma.cu); x in 16-byte pieces.  launch_rot goes there by itself.
 int rot_few_cluster(const RotGeom& g, int64_t M, int n_problems, const RotProblem* problems);      // CTAs of a cluster where it takes few tokens in clusters, or 1
 bool rot_umma_supports(const RotGeom& g, int n_problems, const RotProblem* problems);

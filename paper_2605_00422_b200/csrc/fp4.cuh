@@ -39,6 +39,12 @@ __device__ __forceinline__ uint32_t fp4_codes8(const float (&v)[8]) {
         : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return r;
 }
+// Two values, the first in the low half of a byte.
+__device__ __forceinline__ uint32_t fp4_codes2(float lo, float hi) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 a;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tmov.b32 %0, {a, a, a, a};\n\t}" : "=r"(r) : "f"(lo), "f"(hi));
+    return r & 0xFFu;
+}
 // ... and back (exact)
 __device__ __forceinline__ void fp4_values8(uint32_t codes, float (&v)[8]) {
     uint32_t h[4];

@@ -29,28 +29,38 @@ struct bwla_fp4_layer {
 
 namespace bwla {
 
-// What the rotation needs beside its outputs
+// What the rotation needs beside its outputs: status words, and room for its fp32 outputs (with 8-bit codes and scales that nobody reads) where
+// a call may go to a kernel that has no microscaled codes.
 struct Fp4RotLayout { size_t y, scales, codes, total; };
-static Fp4RotLayout rot_layout_of(int64_t M, int64_t K) {
+static Fp4RotLayout rot_layout_of(const RotGeom& g, int64_t M) {
     Fp4RotLayout w{};
-    w.y = kStatusBytes;
-    w.scales = w.y + align_up((size_t)M * (size_t)K * 4, 256);
+    w.y = w.scales = w.codes = w.total = kStatusBytes;
+    if (!rot_fp4_unfused(g)) return w;
+    w.scales = w.y + align_up((size_t)M * (size_t)g.K * 4, 256);
     w.codes = w.scales + align_up((size_t)M * 4, 256);
-    w.total = w.codes + align_up((size_t)M * (size_t)K, 256);
+    w.total = w.codes + align_up((size_t)M * (size_t)g.K, 256);
     return w;
 }
 
 // chained: the outputs are scratch of the call, read by a kernel that waits for this one
-static int rotate_quant(const PreparedFactors& f, const float* P1, const float* P2, int64_t K, const void* x, int64_t M, int64_t ldx, int format,
+static int rotate_quant(const PreparedFactors& f, const float* P1, const float* P2, const void* x, int64_t M, int64_t ldx, int format,
                         uint8_t* codes, uint8_t* scales, float* row_scales, void* workspace, bool chained, cudaStream_t stream) {
-    const Fp4RotLayout w = rot_layout_of(M, K);
     char* base = (char*)workspace;
     RotProblem pr{};
     pr.prepared = f.base; pr.many = f.many; pr.P1 = P1; pr.P2 = P2;
-    pr.codes = (int8_t*)(base + w.codes); pr.scales = (float*)(base + w.scales); pr.y = (float*)(base + w.y);
-    const int st = launch_rot(f.geom, x, M, ldx, 8, 0, 1, &pr, nullptr, (uint32_t*)base, stream);
+    pr.fp4 = format == BWLA_FP4_NV ? 2 : 1; pr.hold = !chained;
+    pr.fp4_codes = codes; pr.fp4_scales = scales; pr.fp4_rows = row_scales;
+    bool taken = false;
+    int st = launch_rot_fp4(f.geom, x, M, ldx, pr, (uint32_t*)base, &taken, stream);
+    if (st != BWLA_OK || taken) return st;
+    const Fp4RotLayout w = rot_layout_of(f.geom, M);
+    if (w.codes == w.y) return BWLA_ERR_UNSUPPORTED;          // (rot_fp4_unfused and launch_rot_fp4 would have to disagree)
+    RotProblem y{};
+    y.prepared = f.base; y.many = f.many; y.P1 = P1; y.P2 = P2;
+    y.codes = (int8_t*)(base + w.codes); y.scales = (float*)(base + w.scales); y.y = (float*)(base + w.y);
+    st = launch_rot(f.geom, x, M, ldx, 8, 0, 1, &y, nullptr, (uint32_t*)base, stream);
     if (st != BWLA_OK) return st;
-    return launch_fp4_quantize(pr.y, BWLA_DTYPE_F32, M, K, K, format, codes, scales, row_scales, chained, stream);
+    return launch_fp4_quantize(y.y, BWLA_DTYPE_F32, M, f.geom.K, f.geom.K, format, codes, scales, row_scales, chained, stream);
 }
 
 }  // namespace bwla
@@ -105,9 +115,10 @@ int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const f
                            (cudaStream_t)stream);
 }
 
-size_t bwla_rotate_quant_fp4_workspace_bytes(int64_t M, int64_t K) {
-    if (!valid_rows(M, K, BWLA_FP4_MX) || K > 25600) return 0;
-    return rot_layout_of(M, K).total;
+size_t bwla_rotate_quant_fp4_workspace_bytes(int64_t M, int64_t K, int n1, int n2) {
+    RotGeom g;
+    if (!valid_rows(M, K, BWLA_FP4_MX) || !valid_rotation_dims(K, n1, n2) || !rot_geometry(n1, n2, &g)) return 0;
+    return rot_layout_of(g, M).total;
 }
 
 int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const float* P1, int n1, const float* P2, int n2, int format,
@@ -118,12 +129,13 @@ int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx,
     if (!x_bf16 || !P1 || !P2 || !codes || !scales || (format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales) || !aligned16(P1) ||
         !aligned16(P2))
         return BWLA_ERR_INVALID_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < bwla_rotate_quant_fp4_workspace_bytes(M, K)) return BWLA_ERR_WORKSPACE;
+    PreparedFactors f{};
+    const bool supported = rot_geometry(n1, n2, &f.geom);
+    if (!workspace || ((uintptr_t)workspace & 255) || (supported && workspace_bytes < rot_layout_of(f.geom, M).total)) return BWLA_ERR_WORKSPACE;
     const int st = check_device();
     if (st != BWLA_OK) return st;
-    PreparedFactors f{};
-    if (!rot_geometry(n1, n2, &f.geom)) return BWLA_ERR_UNSUPPORTED;
-    return rotate_quant(f, P1, P2, K, x_bf16, M, ldx, format, codes, scales, row_scales, workspace, false, (cudaStream_t)stream);
+    if (!supported) return BWLA_ERR_UNSUPPORTED;
+    return rotate_quant(f, P1, P2, x_bf16, M, ldx, format, codes, scales, row_scales, workspace, false, (cudaStream_t)stream);
 }
 
 size_t bwla_fp4_layer_prepared_bytes(int64_t K, int n1, int n2) {
@@ -155,7 +167,7 @@ int bwla_fp4_layer_create(bwla_fp4_layer** layer, int64_t K, int64_t N, const fl
 void bwla_fp4_layer_destroy(bwla_fp4_layer* layer) { free(layer); }
 
 // [rotation][codes][scales][row scales]
-static size_t layer_codes_at(const bwla_fp4_layer* L, int64_t M) { return rot_layout_of(M, L->K).total; }
+static size_t layer_codes_at(const bwla_fp4_layer* L, int64_t M) { return rot_layout_of(L->factors.geom, M).total; }
 static size_t layer_scales_at(const bwla_fp4_layer* L, int64_t M) { return layer_codes_at(L, M) + align_up((size_t)M * (size_t)(L->K / 2), 256); }
 static size_t layer_rows_at(const bwla_fp4_layer* L, int64_t M) { return layer_scales_at(L, M) + align_up(bwla_fp4_scale_bytes(M, L->K, L->format), 256); }
 
@@ -170,10 +182,10 @@ int bwla_fp4_layer_rotate_quant(const bwla_fp4_layer* L, const void* x_bf16, int
     if (!L || M < 0 || M > kFp4MaxRows || ldx < L->K) return BWLA_ERR_INVALID_ARG;
     if (M == 0) return BWLA_OK;
     if (!x_bf16 || !codes || !scales || (L->format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales)) return BWLA_ERR_INVALID_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < bwla_rotate_quant_fp4_workspace_bytes(M, L->K)) return BWLA_ERR_WORKSPACE;
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < rot_layout_of(L->factors.geom, M).total) return BWLA_ERR_WORKSPACE;
     const int st = check_device();
     if (st != BWLA_OK) return st;
-    return rotate_quant(L->factors, L->P1, L->P2, L->K, x_bf16, M, ldx, L->format, codes, scales, row_scales, workspace, false, (cudaStream_t)stream);
+    return rotate_quant(L->factors, L->P1, L->P2, x_bf16, M, ldx, L->format, codes, scales, row_scales, workspace, false, (cudaStream_t)stream);
 }
 
 int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M, int64_t ldx, void* out_bf16, int64_t ldo, void* workspace,
@@ -189,7 +201,7 @@ int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M
     uint8_t* codes = (uint8_t*)(base + layer_codes_at(L, M));
     uint8_t* scales = (uint8_t*)(base + layer_scales_at(L, M));
     float* rows = L->format == BWLA_FP4_NV ? (float*)(base + layer_rows_at(L, M)) : nullptr;
-    st = rotate_quant(L->factors, L->P1, L->P2, L->K, x_bf16, M, ldx, L->format, codes, scales, rows, workspace, true, (cudaStream_t)stream);
+    st = rotate_quant(L->factors, L->P1, L->P2, x_bf16, M, ldx, L->format, codes, scales, rows, workspace, true, (cudaStream_t)stream);
     if (st != BWLA_OK) return st;
     return launch_fp4_gemm(Fp4GemmArgs{codes, scales, rows, L->w_codes, L->w_scales, L->w_rows, M, L->K, L->N, L->format, (__nv_bfloat16*)out_bf16, ldo,
                                        (uint32_t*)workspace},

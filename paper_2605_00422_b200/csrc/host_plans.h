@@ -228,6 +228,16 @@ inline bool rot_rows_crowded(const RotGeom& g, bool t_first, int64_t t, int few_
     return t <= 16 || t > 64 || (behind < sms - 2 && behind + (t + 1) / 2 <= sms + 24);
 }
 
+// Microscaled 4-bit codes on mma.sync: 16 neighbouring values have to be one warp's rows (n2 a multiple of 16), and a group keeps its rows of Y, and
+// an exponent for every 16 values of two tokens, in shared memory, for which there may be room beside fewer groups only.
+BWLA_HOST_DEVICE inline int rot_fp4_row(const RotGeom& g) { return g.dtc * 16 + 4; }
+BWLA_HOST_DEVICE inline int rot_fp4_group_bytes(const RotGeom& g) { return (g.n1 * rot_fp4_row(g) * 4 + 2 * (g.K >> 4) + 15) / 16 * 16; }
+inline bool rot_fp4_groups(const RotGeom& g, int* groups) {
+    if (g.n2 % 16 != 0) return false;
+    while (*groups > 1 && g.group_off + *groups * (g.group_bytes + rot_fp4_group_bytes(g)) > kRotMaxSmem) --*groups;
+    return g.group_off + *groups * (g.group_bytes + rot_fp4_group_bytes(g)) <= kRotMaxSmem;
+}
+
 // ---- rotation of many tokens on tcgen05 (rot_umma.cu) ----
 constexpr int kRotUmmaSharedBytes = 1792;      // its barriers and small per-CTA state
 struct RotUmmaGeom {
@@ -290,13 +300,14 @@ struct RotRowsGeom {
     int xb;                 // buffers of x
     int staged, out_bytes;  // outputs of a step go through shared memory (two buffers of out_bytes)
     int p1_off, x_off, st_off, sh_off, total;   // the terms of P2^T at 0
+    int exps;               // bytes of the exponents that threads exchange for microscaled 4-bit codes
 };
 // What follows the factors, with xb buffers of x.
 inline bool rot_rows_places(RotRowsGeom& g, int xb, int x_terms) {
     g.xb = xb;
     g.st_off = g.x_off + xb * x_terms * g.atoms2 * 128 * 64;
     g.sh_off = (g.st_off + (g.staged ? 2 * g.out_bytes : 0) + 127) / 128 * 128;
-    g.total = g.sh_off + kRotRowsSharedBytes;
+    g.total = g.sh_off + kRotRowsSharedBytes + g.exps;
     return g.total <= kRotMaxSmem;
 }
 // n1 in (32, 128] on the lanes; n2 a multiple of 16 up to 128: two accumulators for either contraction fill four (or six, up to 80
@@ -321,6 +332,19 @@ inline bool rot_rows_geometry(int n1, int n2, int out_size, RotRowsGeom* out, in
     for (int xb = x_terms == 1 ? 2 : 1; xb >= 1; --xb)
         if (rot_rows_places(g, xb, x_terms)) { *out = g; return true; }
     return false;
+}
+// For microscaled 4-bit codes, which leave in 8-byte pieces from registers: no outputs in shared memory, an exponent for every 16 values of two steps.
+inline bool rot_rows_fp4(RotRowsGeom& g) {
+    g.staged = 0;
+    g.exps = (2 * g.tps * (g.K / 16) + 15) / 16 * 16;
+    return rot_rows_places(g, g.xb, 1) || rot_rows_places(g, 1, 1);
+}
+// Whether a call for microscaled codes may go to a kernel that has none, and needs room for the rotated values
+inline bool rot_fp4_unfused(const RotGeom& g) {
+    RotRowsGeom rows;
+    int groups = 1;
+    const bool mma = rot_fp4_groups(g, &groups), many = rot_rows_geometry(g.n1, g.n2, 1, &rows) && rot_rows_fp4(rows);
+    return !mma || (!many && !rot_mma_always(g));
 }
 // Whether rows of weights are binarised there and not by rot_mma.cu: up to 80 columns (its error is smaller then), more rows than half of the SMs, and
 // factors for which a step, whose time does not depend on n1, is the shorter one.  us of 4000 to 5120 rows, rot_mma.cu | rot_rows.cu, fp32 and bf16:

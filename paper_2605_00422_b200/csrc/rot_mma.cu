@@ -31,12 +31,13 @@
 #include <type_traits>
 
 #include "bwla_common.cuh"
+#include "fp4.cuh"
 #include "prologue_roles.cuh"
 #include "rot_mma.cuh"
 
 namespace bwla {
 
-enum { kRotQuant = 0, kRotBf16 = 1, kRotBinarize = 2, kRotDigits = 3 };
+enum { kRotQuant = 0, kRotBf16 = 1, kRotBinarize = 2, kRotDigits = 3, kRotMx = 4, kRotNv = 5 };      // (the last two: microscaled 4-bit codes)
 
 // What the warps and CTAs of a token exchange: one per group, behind its operand tiles.  [token parity][warp of the token]
 struct RotShared {
@@ -81,6 +82,7 @@ struct RotKernelParams {
     int bits, asym;
     int n_problems;
     int clusters_per_problem;       // group i of a problem (counted over its clusters) takes tokens i, i + all groups, ...
+    int fp4_off;                    // microscaled 4-bit codes: the groups' rows of Y and exponents
     int rot_first, rot_ctas;        // rotation CTAs are blocks [rot_first, rot_first + rot_ctas)
     RotProblem prob[kRotMaxProblems];
     uint32_t* status;
@@ -127,6 +129,12 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
     uint8_t* const p1s = smem + g.p1_off;
     uint8_t* const xs = gs;
     uint8_t* const zs = gs + g.z_rel;
+    // microscaled 4-bit codes: this CTA's rows of Y, [c][d], rows of y_row words (four more than a multiple of 16: stores and reads miss each
+    // other's banks); MX: exponents, [token parity][K / 16]
+    const int y_row = rot_fp4_row(g), y_tiles = min(g.dtc, (g.n2 >> 4) - rank * g.dtc);
+    uint8_t* const fp4_mem = smem + p.fp4_off + group * rot_fp4_group_bytes(g);
+    float* const ybuf = reinterpret_cast<float*>(fp4_mem);
+    uint8_t* const exps = fp4_mem + g.n1 * y_row * 4;
 
     // ---- the layer's constants (they do not depend on the preceding kernel, except that the factors of a binarisation may be what it has
     //      made), and the zeros around x ----
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
     if (g.dc > 1) { cluster_arrive_release(); cluster_wait_acquire(); }   // every CTA of the cluster runs: its slots may be written
     // (The signs, scales and shifts of a binarisation are constants of the calls behind it, which read constants before they wait: they
     // start when this kernel has ended.)
-    if (MODE != kRotBinarize) griddep_launch_dependents();
+    if (MODE < kRotMx ? MODE != kRotBinarize : !pr.hold) griddep_launch_dependents();
     int ntok = tok0 < p.M ? (int)((p.M - tok0 + stride - 1) / stride) : 0;
     // this thread's chunks of X: tid, tid + T, ...; (row, column) advance without divisions
     const int ch_a0 = tid / cpr, ch_c0 = tid - ch_a0 * cpr, ch_da = T / cpr, ch_dc = T - ch_da * cpr;
@@ -546,6 +554,41 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
             publish(sh.amax[par], __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)));
             if (asym) publish(sh.vmin[par], __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(-vmin, 0.f))));
         }
+        if constexpr (MODE == kRotMx || MODE == kRotNv) {
+            if (live) {
+                // Y by output columns, so that a thread finds 16 neighbouring values (codes straight from the accumulators, a lane with two values
+                // of a column, took 1800 instructions a warp at 64 x 64: 3.5 us a token)
+#pragma unroll
+                for (int j = 0; j < NTW; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (8 * j < lim[i & 1]) ybuf[((nt0 + j) * 8 + 2 * tq + (i & 1)) * y_row + dtl * 16 + gq + 4 * (i & 2)] = acc[j][i];
+                if (MODE == kRotNv) {
+                    uint32_t top = 0u;                // (bits, NaNs included)
+#pragma unroll
+                    for (int j = 0; j < NTW; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(acc[j][i]) & 0x7FFFFFFFu);
+                    publish(sh.amax[par], __reduce_max_sync(0xFFFFFFFFu, top));
+                } else {
+                    // exponents of the largest of 16 values, to all CTAs of the token: a block of 32 may have its halves in two
+                    barrier();
+                    for (int i = tid; i < g.n1 * y_tiles; i += T) {
+                        const int c = i / y_tiles, dl = i - c * y_tiles;
+                        const uint4* at = reinterpret_cast<const uint4*>(ybuf + c * y_row + 16 * dl);
+                        uint32_t m = 0u;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint4 u = at[q];
+                            m = max(max(m, max(u.x & 0x7FFFFFFFu, u.y & 0x7FFFFFFFu)), max(u.z & 0x7FFFFFFFu, u.w & 0x7FFFFFFFu));
+                        }
+                        const uint32_t to = smem_u32(exps + par * (g.K >> 4) + ((c * g.n2 + rank * g.dtc * 16) >> 4) + dl);
+                        if (g.dc == 1) st_shared_u8(to, m >> 23);
+                        else for (int r = 0; r < g.dc; ++r) st_shared_cluster_u8(map_shared_rank(to, (uint32_t)r), m >> 23);
+                    }
+                }
+            }
+        }
         if (MODE == kRotDigits && live) {
             // the values of the weight-only operating point are bf16; their largest magnitude as bits, NaNs included
             uint32_t top = 0u;
@@ -708,6 +751,60 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
                 if (lane == 0 && local != 0) atomicAdd(&sh.qsum[par][pl], local);
             }
             if (tid == 0 && rank == 0) pr.scales[t] = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : pow2f(es2 - es) * pow2f(-es2);
+        } else if constexpr (MODE == kRotMx || MODE == kRotNv) {
+            // microscaled 4-bit codes (fp4.cuh), 16 neighbouring values a thread
+            constexpr bool MICRO16 = MODE == kRotNv;
+            const uint32_t top = MICRO16 ? slots_max(sh.amax[par]) : 0u;
+            const bool bad = top >= 0x7F800000u;
+            const int E = bad ? 0 : fp4_row_exponent(__uint_as_float(top));
+            const float to_row = fp4_pow2(-E);
+            const int64_t col_tiles = (g.K / (MICRO16 ? 16 : 32) + 3) / 4;
+            uint8_t* const scales = pr.fp4_scales + fp4_scale_at(t, 0, col_tiles);
+            auto put_scale = [&](int j, uint32_t byte) { scales[(j >> 2) * 512 + (j & 3)] = (uint8_t)byte; };
+            if (rank == 0 && warp == 0) {                     // the token's scalars, and the blocks that fill the last tile
+                if (MICRO16 && lane == 0) pr.fp4_rows[t] = bad ? __int_as_float(0x7FC00000) : fp4_pow2(E);
+                const int j = g.K / (MICRO16 ? 16 : 32) + lane;
+                if (j < 4 * (int)col_tiles) put_scale(j, 0u);
+            }
+            uint2* const ct = reinterpret_cast<uint2*>(pr.fp4_codes + t * (int64_t)(g.K >> 1));
+#pragma unroll 1
+            for (int i = tid; i < g.n1 * y_tiles; i += T) {
+                const int c = i / y_tiles, dl = i - c * y_tiles, k16 = ((c * g.n2 + rank * g.dtc * 16) >> 4) + dl;
+                const float4* at = reinterpret_cast<const float4*>(ybuf + c * y_row + 16 * dl);
+                float f[2][8];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 u = at[q];
+                    f[q >> 1][4 * (q & 1)] = u.x; f[q >> 1][4 * (q & 1) + 1] = u.y; f[q >> 1][4 * (q & 1) + 2] = u.z; f[q >> 1][4 * (q & 1) + 3] = u.w;
+                }
+                Fp4Block b;
+                if (MICRO16) {
+                    uint32_t m = 0u;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) m = max(m, __float_as_uint(f[e >> 3][e & 7]) & 0x7FFFFFFFu);
+                    b = fp4_block_nv<true>(bad ? 0.f : __uint_as_float(m), to_row);
+                    put_scale(k16, b.byte);
+                } else {
+                    const uint16_t two = *reinterpret_cast<const volatile uint16_t*>(exps + par * (g.K >> 4) + (k16 & ~1));
+                    b = fp4_block_mx(__uint_as_float(max((uint32_t)two & 0xFFu, (uint32_t)two >> 8) << 23));
+                    if ((k16 & 1) == 0) put_scale(k16 >> 1, b.byte);
+                }
+                uint32_t word[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (MICRO16) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[h][e] = __fmul_rn(f[h][e], to_row);
+                        fp4_divide8<true>(f[h], b, b.inv, 1.f);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[h][e] = __fmul_rn(f[h][e], b.mul);
+                    }
+                    word[h] = fp4_codes8(f[h]);
+                }
+                const bool none = MICRO16 ? bad : b.byte == 255u;
+                ct[k16] = none ? make_uint2(0u, 0u) : make_uint2(word[0], word[1]);
+            }
         } else if (MODE == kRotBf16) {
             // the weight-only operating point: bf16 values (layout 1: inside each group of 32, position 2 (k % 16) +
             // (k % 32) / 16), and where asked for their sum
@@ -779,7 +876,7 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
         barrier();
         flush_qsum(tok0 + (int64_t)(ntok - 1) * stride, (ntok - 1) & 1);
     }
-    if (MODE == kRotBinarize) __threadfence();       // (see above: complete in memory, not only issued)
+    if (MODE == kRotBinarize || (MODE >= kRotMx && pr.hold)) __threadfence();       // (see above: complete in memory, not only issued)
     // nobody leaves while a neighbour may still store into its shared memory
     if (g.dc > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
 }
@@ -871,6 +968,7 @@ static int launch_rot_kernel(RotKernel k, const RotGeom& g, RotKernelParams& p, 
 }
 
 static RotKernel rot_kernel_of(const RotGeom& g, const RotProblem& pr) {
+    if (pr.fp4) return pr.fp4 == 2 ? pick_kernel<kRotNv, false>(g) : pick_kernel<kRotMx, false>(g);
     return pr.yhat ? pick_kernel<kRotBf16, false>(g) : pr.digits ? pick_kernel<kRotDigits, false>(g) : pick_kernel<kRotQuant, false>(g);
 }
 
@@ -991,6 +1089,41 @@ int launch_rot(const RotGeom& base, const void* x, int64_t M, int64_t ldx, int b
     }
     for (int i = n_problems; i <= kRotMaxProblems; ++i) p.lr_begin[i] = lr_total;
     return launch_rot_kernel(rot_kernel_of(g, problems[0]), g, p, smem, lr_total, stream);
+}
+
+int launch_rot_fp4(const RotGeom& base, const void* x, int64_t M, int64_t ldx, const RotProblem& problem, uint32_t* status, bool* taken,
+                   cudaStream_t stream) {
+    if (M >= ((int64_t)1 << 31)) return BWLA_ERR_INVALID_ARG;
+    const bool vec = rot_accepts_x(x, ldx);
+    *taken = true;
+    RotGeom g = base;
+    const bool few = few_geometry(base, M, 1, &problem, &g);
+    int groups = choose_groups(g, M, 1);
+    bool mma = rot_fp4_groups(g, &groups);
+    if (!mma && few) {
+        g = base;
+        groups = choose_groups(g, M, 1);
+        mma = rot_fp4_groups(g, &groups);
+    }
+    mma = mma && (few || !vec || rot_mma_always(base));
+    // (as launch_rot has it for codes: many tokens on rot_rows.cu where it can and is the faster one)
+    RotRowsGeom rows;
+    const bool can = vec && rot_rows_supports(base, 1, &problem) && rot_rows_geometry(base.n1, base.n2, 1, &rows) && rot_rows_fp4(rows);
+    const bool faster = few ? !rot_mma_always(base) : rot_rows_faster(base, false, !problem.prepared, false, false, M, sm_count());
+    if (can && (!mma || faster)) {
+        const OktLowrank none{};
+        return launch_rot_rows(base, x, M, ldx, 8, 0, 1, &problem, &none, status, stream);
+    }
+    // Factors that many tokens of take to rot_umma.cu or okt_umma.cu, which have no microscaled codes, are faster there with fp32 outputs and the
+    // quantiser behind.
+    *taken = mma;
+    if (!mma) return BWLA_OK;
+    RotKernelParams p{};
+    p.g = g; p.groups = groups;
+    p.fp4_off = g.group_off + groups * g.group_bytes;
+    p.x = x; p.ldx = ldx; p.x_vec = vec; p.M = M; p.bits = 8; p.n_problems = 1; p.status = status;
+    p.prob[0] = problem;
+    return launch_rot_kernel(rot_kernel_of(g, problem), g, p, (size_t)(p.fp4_off + groups * rot_fp4_group_bytes(g)), 0, stream);
 }
 
 int launch_rot_binarize(const RotGeom& g, const void* w, int dtype, int64_t N, int64_t ldw, const RotProblem& problem, uint32_t* status,

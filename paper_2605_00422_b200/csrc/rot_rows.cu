@@ -38,6 +38,7 @@
 #include <type_traits>
 
 #include "bwla_common.cuh"
+#include "fp4.cuh"
 #include "prologue_roles.cuh"
 #include "rot_mma.cuh"
 #include "tensor_map.cuh"
@@ -175,9 +176,9 @@ __device__ __forceinline__ void issue_outputs(bool one, uint32_t y0, uint32_t y1
     issue_y<KS, CHAINS, false>(one, y0, y1, y2, a, b, b_hi, blk, idesc);              // hi hi
 }
 
-// MODE: the symmetric or the asymmetric quantiser, the weight-only operating point, or the binarisation of weight rows.  CH: 16-column
-// chunks of a warp.  F32: x is fp32.
-enum { kRowsSym = 0, kRowsAsym = 1, kRowsBf16 = 2, kRowsBinarize = 3 };
+// MODE: the symmetric or the asymmetric quantiser, the weight-only operating point, the binarisation of weight rows, or microscaled 4-bit
+// codes.  CH: 16-column chunks of a warp.  F32: x is fp32.
+enum { kRowsSym = 0, kRowsAsym = 1, kRowsBf16 = 2, kRowsBinarize = 3, kRowsMx = 4, kRowsNv = 5 };
 template <int MODE, int CH, bool F32 = false>
 __global__ void __launch_bounds__(CH == 1 ? 768 : 640, 1)
 rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ RotRowsParams p) {
@@ -248,7 +249,7 @@ rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sh.tmem_slot);
     if (MODE != kRowsBinarize) {
         // (dependents start when every CTA has its tensor memory: one that got a CTA's columns first would wait for this grid with them)
-        griddep_launch_dependents();
+        if (MODE < kRowsMx || !pr.hold) griddep_launch_dependents();
         griddep_wait();                               // x may be the output of the preceding kernel
     }
     const int n = (MODE == kRowsBinarize || !sh.skip) && first < steps_all ? (int)((steps_all - first + p.ctas_per_problem - 1) / p.ctas_per_problem) : 0;
@@ -342,7 +343,7 @@ rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
         }
     } else if (warp == 3 && MODE != kRowsBinarize) {
         // ---------------- code sums and staged outputs of a step ----------------
-        for (int i = 0; i < n; ++i) {
+        for (int i = 0; i < (MODE < kRowsMx ? n : 0); ++i) {       // (microscaled codes leave from registers)
             const int par = i & 1;
             if (!warp_wait(&sh.out_full[par], (uint32_t)((i >> 1) & 1), abort_flag)) { give_up(p.status, abort_flag, 0x540); break; }
             const int64_t t0 = (first + (int64_t)i * p.ctas_per_problem) * g.tps;
@@ -352,7 +353,7 @@ rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                 uint8_t* dst = MODE == kRowsBf16 ? reinterpret_cast<uint8_t*>(pr.yhat) : reinterpret_cast<uint8_t*>(pr.codes);
                 bulk_s2g(dst + t0 * size, smem + g.st_off + par * g.out_bytes, (uint32_t)(tokens * size));
             }
-            if (MODE != kRowsBf16 && pr.qsum) {
+            if (MODE != kRowsBf16 && MODE < kRowsMx && pr.qsum) {
                 const int tk = lane >> 3, part = lane & 7;
                 static_assert(kQsumParts == 8, "a lane per part");
                 const int sum = tk < 2 ? sh.qsum[par][tk] : 0;
@@ -379,7 +380,10 @@ rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
         // Its columns of Y.  Where rows are whole groups of 32 outputs and a warp has 16 columns, they are those that make 16 (or, of bf16
         // values, 32) neighbouring bytes of the contractions' order: a half of a group, four (eight) columns of every eight (sixteen).
         constexpr int RUN = MODE == kRowsBf16 ? 8 : 4;
-        const bool gather = MODE != kRowsBinarize && CH == 1 && (g.n2 & 31) == 0;
+        const bool gather = MODE < kRowsBinarize && CH == 1 && (g.n2 & 31) == 0;
+        // (microscaled codes: exponents of the largest magnitudes of 16 values, [step parity][token][K / 16], where a block of 32 has two threads)
+        uint8_t* const exps = smem + g.sh_off + kRotRowsSharedBytes;
+        const int per_exps = g.K >> 4;
         const int y0 = gather ? 32 * (wc >> 1) + RUN * (wc & 1) : c0;
         auto column = [&](int e) { return y0 + (gather ? e % RUN + (32 / (16 / RUN)) * (e / RUN) : e); };
         bool ok = true;
@@ -539,7 +543,25 @@ rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                     for (int e = 0; e < NC; ++e) y[e] = y[e] * f1 * f2;
                     f1 = 1.f;
                 }
-                if (MODE == kRowsBf16 || MODE == kRowsBinarize) {
+                if constexpr (MODE == kRowsMx || MODE == kRowsNv) {
+#pragma unroll
+                    for (int e = 0; e < NC; ++e) y[e] *= f1;
+                    f1 = 1.f;
+                    if (MODE == kRowsNv) {
+#pragma unroll
+                        for (int e = 0; e < NC; ++e) top = max(top, __float_as_uint(y[e]) & 0x7FFFFFFFu);
+                        top = __reduce_max_sync(0xFFFFFFFFu, valid ? top : 0u);
+                    } else if (valid) {
+#pragma unroll
+                        for (int ch = 0; ch < CH; ++ch) {
+                            if (16 * ch >= have) break;
+                            uint32_t m = 0u;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) m = max(m, __float_as_uint(y[16 * ch + e]) & 0x7FFFFFFFu);
+                            exps[(par * g.tps + tk) * per_exps + ((c * g.n2 + y0) >> 4) + ch] = (uint8_t)(m >> 23);
+                        }
+                    }
+                } else if (MODE == kRowsBf16 || MODE == kRowsBinarize) {
                     // the sum of the values goes where the quantiser's two extremes go
                     if (MODE == kRowsBinarize || pr.ysum) {
                         double s = 0.0, s1 = 0.0;             // (of the scaled, or the rounded values; two chains)
@@ -562,7 +584,65 @@ rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                     top = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax * f1));
                     if (MODE == kRowsAsym) bottom = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(-vmin * f1, 0.f)));
                 }
-                if (lane == 0) { sh.ymax[par][tk][slot] = top; if (MODE != kRowsSym) sh.ymin[par][tk][slot] = bottom; }
+                if (lane == 0) { sh.ymax[par][tk][slot] = top; if (MODE != kRowsSym && MODE < kRowsMx) sh.ymin[par][tk][slot] = bottom; }
+            };
+            // ---- the step before: microscaled 4-bit codes (fp4.cuh), 16 neighbouring ones at a time
+            auto emit_fp4 = [&](int ze) {
+                const uint32_t s0 = lane < slots ? *reinterpret_cast<volatile uint32_t*>(&sh.ymax[par][tk][lane]) : 0u;
+                const uint32_t top = MODE == kRowsNv ? __reduce_max_sync(0xFFFFFFFFu, s0) : 0u;
+                const bool bad = ze == rr::kNotFinite || top >= 0x7F800000u;
+                if (ok && t < p.M) {
+                    constexpr bool MICRO16 = MODE == kRowsNv;
+                    const int64_t col_tiles = (g.K / (MICRO16 ? 16 : 32) + 3) / 4;
+                    uint8_t* const scales = pr.fp4_scales + fp4_scale_at(t, 0, col_tiles);
+                    auto scale_at = [&](int j) -> uint8_t& { return scales[(size_t)(j >> 2) * 512 + (j & 3)]; };
+                    const int E = bad ? 0 : fp4_row_exponent(__uint_as_float(top));
+                    const float to_row = fp4_pow2(-E);
+                    if (slot == 0) {                              // the token's scalars, and the blocks that fill the last tile
+                        if (MICRO16 && lane == 0) pr.fp4_rows[t] = bad ? __int_as_float(0x7FC00000) : fp4_pow2(E);
+                        const int j = g.K / (MICRO16 ? 16 : 32) + lane;
+                        if (j < 4 * (int)col_tiles) scale_at(j) = 0u;
+                    }
+                    if (valid) {
+                        const int k0 = c * g.n2 + y0;
+#pragma unroll
+                        for (int ch = 0; ch < CH; ++ch) {
+                            if (16 * ch >= have) break;
+                            const int k = k0 + 16 * ch;
+                            Fp4Block b;
+                            if (MICRO16) {
+                                uint32_t m = 0u;
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) m = max(m, __float_as_uint(y[16 * ch + e]) & 0x7FFFFFFFu);
+                                b = fp4_block_nv<true>(bad ? 0.f : __uint_as_float(m), to_row);
+                                scale_at(k >> 4) = (uint8_t)b.byte;
+                            } else {
+                                const uint16_t two = *reinterpret_cast<const uint16_t*>(exps + (par * g.tps + tk) * per_exps + ((k >> 5) << 1));
+                                const uint32_t ex = bad ? 255u : max((uint32_t)two & 0xFFu, (uint32_t)two >> 8);
+                                b = fp4_block_mx(__uint_as_float(ex << 23));
+                                if ((k & 31) == 0) scale_at(k >> 5) = (uint8_t)b.byte;
+                            }
+                            uint32_t word[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float f[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) f[e] = y[16 * ch + 8 * h + e];
+                                if (MICRO16) {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(f[e], to_row);
+                                    fp4_divide8<true>(f, b, b.inv, 1.f);
+                                } else {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(f[e], b.mul);
+                                }
+                                word[h] = fp4_codes8(f);
+                            }
+                            const bool none = MICRO16 ? bad : b.byte == 255u;
+                            *reinterpret_cast<uint2*>(pr.fp4_codes + t * (int64_t)(g.K >> 1) + (k >> 1)) = none ? make_uint2(0u, 0u) : make_uint2(word[0], word[1]);
+                        }
+                    }
+                }
             };
             // ---- the step before: codes, scale and code sum, or bf16 values
             auto emit = [&](int ze) {
@@ -777,17 +857,19 @@ rot_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                 if (i > 0) load_y(ze);
                 token_barrier();
                 if (i < n) convert();
-                if (i > 0) emit(ze);
+                if constexpr (MODE == kRowsMx || MODE == kRowsNv) { if (i > 0) emit_fp4(ze); }
+                else if (i > 0) emit(ze);
             } else {
                 if (i > 0) load_y(ze);
                 if (i < n) load_v();
                 token_barrier();
                 if (i < n) convert();
-                if (i > 0) emit(ze);
+                if constexpr (MODE == kRowsMx || MODE == kRowsNv) { if (i > 0) emit_fp4(ze); }
+                else if (i > 0) emit(ze);
             }
         }
         if (!ok) *abort_flag = 1;
-        if (MODE == kRowsBinarize) __threadfence();   // (see above: complete in memory, not only issued)
+        if (MODE == kRowsBinarize || (MODE >= kRowsMx && pr.hold)) __threadfence();   // (see above: complete in memory, not only issued)
     }
     tc_fence_before();
     __syncthreads();
@@ -847,6 +929,7 @@ int launch_rot_rows(const RotGeom& base, const void* x, int64_t M, int64_t ldx, 
     RotRowsParams p{};
     if (!rot_rows_geometry(base.n1, base.n2, problems[0].yhat ? 2 : 1, &p.g)) return BWLA_ERR_INVALID_ARG;
     const RotRowsGeom& g = p.g;
+    if (problems[0].fp4) rot_rows_fp4(p.g);
     p.M = M; p.bits = bits; p.n_problems = n_problems; p.status = status;
     for (int i = 0; i < n_problems; ++i) p.prob[i] = problems[i];
     CUtensorMap xm;
@@ -855,7 +938,8 @@ int launch_rot_rows(const RotGeom& base, const void* x, int64_t M, int64_t ldx, 
     static const RotRowsKernel kernels[3][2] = {{rot_rows_kernel<kRowsSym, 1>, rot_rows_kernel<kRowsSym, 2>},
                                          {rot_rows_kernel<kRowsAsym, 1>, rot_rows_kernel<kRowsAsym, 2>},
                                          {rot_rows_kernel<kRowsBf16, 1>, rot_rows_kernel<kRowsBf16, 2>}};
-    const RotRowsKernel k = kernels[problems[0].yhat ? kRowsBf16 : asym ? kRowsAsym : kRowsSym][g.chunks - 1];
+    static const RotRowsKernel fp4[2][2] = {{rot_rows_kernel<kRowsMx, 1>, rot_rows_kernel<kRowsMx, 2>}, {rot_rows_kernel<kRowsNv, 1>, rot_rows_kernel<kRowsNv, 2>}};
+    const RotRowsKernel k = problems[0].fp4 ? fp4[problems[0].fp4 - 1][g.chunks - 1] : kernels[problems[0].yhat ? kRowsBf16 : asym ? kRowsAsym : kRowsSym][g.chunks - 1];
     int lr_blocks = 0;
     size_t lr_smem = 0;
     for (int i = 0; i < n_problems; ++i) {
