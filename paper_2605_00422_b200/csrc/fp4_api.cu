@@ -96,7 +96,7 @@ int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const floa
 
 size_t bwla_fp4_gemm_workspace_bytes(int64_t M, int64_t K, int64_t N) {
     if (!valid_rows(M, K, BWLA_FP4_MX) || !valid_rows(N, K, BWLA_FP4_MX)) return 0;
-    return kStatusBytes;
+    return kStatusBytes + fp4_gemm_part_bytes(M, K, N);
 }
 
 int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_rows, int64_t M, int64_t K, const uint8_t* w_codes,
@@ -111,7 +111,8 @@ int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const f
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < bwla_fp4_gemm_workspace_bytes(M, K, N)) return BWLA_ERR_WORKSPACE;
     const int st = check_device();
     if (st != BWLA_OK) return st;
-    return launch_fp4_gemm(Fp4GemmArgs{a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, M, K, N, format, (__nv_bfloat16*)out_bf16, ldo, (uint32_t*)workspace},
+    return launch_fp4_gemm(Fp4GemmArgs{a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, M, K, N, format, (__nv_bfloat16*)out_bf16, ldo, (uint32_t*)workspace,
+                                       (float*)((char*)workspace + kStatusBytes), fp4_gemm_part_bytes(M, K, N)},
                            (cudaStream_t)stream);
 }
 
@@ -166,14 +167,16 @@ int bwla_fp4_layer_create(bwla_fp4_layer** layer, int64_t K, int64_t N, const fl
 
 void bwla_fp4_layer_destroy(bwla_fp4_layer* layer) { free(layer); }
 
-// [rotation][codes][scales][row scales]
+// [rotation][codes][scales][row scales][sums of parts of tiles]
 static size_t layer_codes_at(const bwla_fp4_layer* L, int64_t M) { return rot_layout_of(L->factors.geom, M).total; }
 static size_t layer_scales_at(const bwla_fp4_layer* L, int64_t M) { return layer_codes_at(L, M) + align_up((size_t)M * (size_t)(L->K / 2), 256); }
 static size_t layer_rows_at(const bwla_fp4_layer* L, int64_t M) { return layer_scales_at(L, M) + align_up(bwla_fp4_scale_bytes(M, L->K, L->format), 256); }
 
+static size_t layer_parts_at(const bwla_fp4_layer* L, int64_t M) { return layer_rows_at(L, M) + align_up((size_t)M * 4, 256); }
+
 size_t bwla_fp4_layer_workspace_bytes(const bwla_fp4_layer* L, int64_t M) {
     if (!L || M < 0 || M > kFp4MaxRows) return 0;
-    return layer_rows_at(L, M) + align_up((size_t)M * 4, 256);
+    return layer_parts_at(L, M) + fp4_gemm_part_bytes(M, L->K, L->N);
 }
 
 int bwla_fp4_layer_rotate_quant(const bwla_fp4_layer* L, const void* x_bf16, int64_t M, int64_t ldx, uint8_t* codes, uint8_t* scales, float* row_scales,
@@ -204,7 +207,7 @@ int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M
     st = rotate_quant(L->factors, L->P1, L->P2, x_bf16, M, ldx, L->format, codes, scales, rows, workspace, true, (cudaStream_t)stream);
     if (st != BWLA_OK) return st;
     return launch_fp4_gemm(Fp4GemmArgs{codes, scales, rows, L->w_codes, L->w_scales, L->w_rows, M, L->K, L->N, L->format, (__nv_bfloat16*)out_bf16, ldo,
-                                       (uint32_t*)workspace},
+                                       (uint32_t*)workspace, (float*)(base + layer_parts_at(L, M)), fp4_gemm_part_bytes(M, L->K, L->N)},
                            (cudaStream_t)stream);
 }
 

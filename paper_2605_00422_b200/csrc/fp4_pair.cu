@@ -9,8 +9,14 @@
 //   warps 2..5   epilogue: accumulators to registers, row scales, bf16, shared memory, bulk tensor stores
 // Tensor memory holds two accumulators of 256 columns that share 96 (512 columns less the scales' 96): tile i + 1 starts when the epilogue has
 // taken the shared ones of tile i into registers, which it does first.
+// The tiles that do not fill the last round, and those of the round before, are cut by k so that every pair has the same number of
+// k-blocks (1024 tokens 25600 -> 5120: 80 tiles on 74 pairs).  A pair that has part of a tile leaves its fp32 sums in the workspace; the last
+// one to arrive adds them, in the order of k, so a call repeats itself bit for bit and nobody waits.
 // What the issuer waits for arrives on barriers of the even CTA, from both; its commits arrive in both.  Every wait is bounded.
+#include <type_traits>
+
 #include "fp4.cuh"
+#include "rot_mma.cuh"
 #include "tensor_map.cuh"
 #include "umma_wait.cuh"
 
@@ -27,7 +33,8 @@ struct Sizes {
     static constexpr int stage = 2 * half_bytes + sa_bytes + sw_bytes;
     static constexpr int out_off = kStages * stage;
     static constexpr int bars_off = out_off + 4 * kStageOut * 2048;
-    static constexpr int total = bars_off + (2 * kStages + 2) * 8 + 16 + 1024;
+    static constexpr int total = bars_off + (2 * kStages + 3) * 8 + 16 + 1024;
+    static_assert(kHalf * kRows * 4 <= kStages * stage, "the sums of a part of a tile lie where the stages were");
     static_assert(total <= 232448, "shared memory");
 };
 // accumulators at columns 0 and 160, then two buffers of scales
@@ -36,6 +43,9 @@ constexpr int kSecond = 160, kShared = 96, kScaleCol = 416;
 
 struct Fp4PairParams {
     int M, N, kblocks, tok_tiles, row_tiles, group;
+    int whole, cut;                  // whole tiles a pair takes before its share of the rest; whether that is cut by k
+    float* parts;                    // [pair][2][CTA of the pair][64][128][4] sums of parts of tiles: one that begins, one that does not begin a tile
+    uint32_t* counters;              // arrivals at a cut tile: a byte for each pair that begins one and CTA
     const float *a_rows, *w_rows;
     __nv_bfloat16* out; int64_t ldo;
     int bulk;                        // rows of out in 16-byte pieces
@@ -43,9 +53,21 @@ struct Fp4PairParams {
 };
 struct Fp4PairMaps { Fp4Maps in; CUtensorMap out; };
 
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* src, int x, int y) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];\n\tcp.async.bulk.commit_group;"
-                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(ptx::smem_u32(src)), "r"(x), "r"(y) : "memory");
+// What one lane of an epilogue warp does, without a branch: behind one the compiler has let the lane and the others run through the code
+// that follows each by itself (four times the instructions, 142 us for 50).
+__device__ __forceinline__ void tma_store_2d_if(bool one, const CUtensorMap* map, const void* src, int x, int y) {      // a group of every lane
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %4, 0;\n\t"
+        "@q cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];\n\tcp.async.bulk.commit_group;\n\t}"
+        ::"l"(reinterpret_cast<uint64_t>(map)), "r"(ptx::smem_u32(src)), "r"(x), "r"(y), "r"((uint32_t)one) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_pair_if(bool one, uint32_t cluster_addr) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}" ::"r"(cluster_addr), "r"((uint32_t)one) : "memory");
+}
+__device__ __forceinline__ uint32_t atomic_add_if(bool one, uint32_t* at, uint32_t v) {
+    uint32_t before = 0u;
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %3, 0;\n\t@q atom.global.add.u32 %0, [%1], %2;\n\t}" : "+r"(before) : "l"(at), "r"(v), "r"((uint32_t)one) : "memory");
+    return before;
 }
 
 template <bool NV>
@@ -62,20 +84,39 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
     uint64_t* empty = full + kStages;
     uint64_t* d_full = empty + kStages;      // the tile's MMAs have completed
     uint64_t* acc_free = d_full + 1;         // the epilogue has the shared columns in registers (and is through with the tile before)
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_free + 1);
+    uint64_t* sums_full = acc_free + 1;      // the sums of the other part of the last tile have landed
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sums_full + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    volatile int* arrived_last = reinterpret_cast<volatile int*>(tmem_slot + 2);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
     const int tiles = p.tok_tiles * p.row_tiles;
-    const int my_tiles = pair < tiles ? (tiles - pair + pairs - 1) / pairs : 0;
+    // pieces of this pair: whole tiles pair, pair + pairs, ..., then the k-blocks [s0, s1) of the tiles behind those, counted through
+    const int64_t rest = (int64_t)(tiles - p.whole * pairs) * p.kblocks;
+    const int rest_tiles = tiles - p.whole * pairs;
+    const int s0 = p.cut ? (int)(rest * pair / pairs) : min(pair, rest_tiles) * p.kblocks;
+    const int s1 = p.cut ? (int)(rest * (pair + 1) / pairs) : min(pair + 1, rest_tiles) * p.kblocks;
+    const int first_tile = s0 / p.kblocks;
+    const int my_tiles = p.whole + (s1 > s0 ? (s1 + p.kblocks - 1) / p.kblocks - first_tile : 0);
     // groups of token tiles, in a group the token tile fastest: what runs at once shares tokens and weights in the L2
-    auto tile_at = [&](int i, int& t0, int& n0) {
-        int g = pair + i * pairs;
+    struct Piece { int t0, n0, kb0, kb1, rest_tile; };
+    auto piece_at = [&](int i) {
+        Piece r;
+        int g;
+        if (i < p.whole) {
+            g = pair + i * pairs; r.rest_tile = 0; r.kb0 = 0; r.kb1 = p.kblocks;
+        } else {
+            r.rest_tile = first_tile + i - p.whole;
+            g = p.whole * pairs + r.rest_tile;
+            const int begin = r.rest_tile * p.kblocks;
+            r.kb0 = max(s0 - begin, 0); r.kb1 = min(s1 - begin, p.kblocks);
+        }
         const int per = p.group * p.row_tiles, first = g / per * p.group, width = min(p.group, p.tok_tiles - first);
         g -= g / per * per;
-        t0 = (first + g % width) * kTok;
-        n0 = (g / width) * kRows;
+        r.t0 = (first + g % width) * kTok;
+        r.n0 = (g / width) * kRows;
+        return r;
     };
 
     if (threadIdx.x == 0) {
@@ -83,6 +124,7 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
         for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
         mbar_init(d_full, 1);
         mbar_init(acc_free, 8);
+        mbar_init(sums_full, 1);
         fence_barrier_init();
         fence_proxy_async();
     }
@@ -101,7 +143,7 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
 
     if (warp == 0) {
         if (elect_one()) {
-            int t0, n0, s = 0;
+            int s = 0;
             uint32_t ph = 1;
             auto weights = [&](int kb, int n0, int s) {
                 if (rank == 0) mbar_expect_tx(&full[s], 2 * S::stage);
@@ -112,21 +154,22 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
                 tma_load_2d_pair(abuf + s * S::half_bytes, &maps.in.a, kb * 128, t0 + rank * kHalf, issuer(&full[s]));
                 tma_load_3d_pair(sabuf + s * S::sa_bytes, &maps.in.a_scales, 0, kb * S::atoms, (t0 >> 7) + rank, issuer(&full[s]));
             };
-            const int ahead = my_tiles > 0 ? min(p.kblocks, kStages) : 0;
-            if (ahead > 0) {
-                tile_at(0, t0, n0);
-                for (int kb = 0; kb < ahead; ++kb) weights(kb, n0, kb);
+            int ahead = 0;
+            if (my_tiles > 0) {
+                const Piece r = piece_at(0);
+                ahead = min(r.kb1 - r.kb0, kStages);
+                for (int j = 0; j < ahead; ++j) weights(r.kb0 + j, r.n0, j);
+                griddep_wait();
+                for (int j = 0; j < ahead; ++j) tokens(r.kb0 + j, r.t0, j);
             }
-            griddep_wait();
-            for (int kb = 0; kb < ahead; ++kb) tokens(kb, t0, kb);
             s = ahead % kStages;
             if (ahead == kStages) ph = 0;
             for (int i = 0; i < my_tiles && !*abort_flag; ++i) {
-                tile_at(i, t0, n0);
-                for (int kb = i == 0 ? ahead : 0; kb < p.kblocks; ++kb) {
+                const Piece r = piece_at(i);
+                for (int kb = r.kb0 + (i == 0 ? ahead : 0); kb < r.kb1; ++kb) {
                     if (!wait_or_abort(&empty[s], ph, abort_flag)) { give_up(p.status, abort_flag, 0x410); break; }
-                    weights(kb, n0, s);
-                    tokens(kb, t0, s);
+                    weights(kb, r.n0, s);
+                    tokens(kb, r.t0, s);
                     if (++s == kStages) { s = 0; ph ^= 1; }
                 }
             }
@@ -145,7 +188,8 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
                 // the columns that this accumulator shares with the tile before
                 if (i >= 1 && !wait_or_abort(acc_free, (uint32_t)((i - 1) & 1), abort_flag)) { give_up(p.status, abort_flag, 0x420); ok = false; break; }
                 const uint32_t d = tmem + (i & 1) * kSecond;
-                for (int kb = 0; kb < p.kblocks; ++kb) {
+                const Piece r = piece_at(i);
+                for (int kb = r.kb0; kb < r.kb1; ++kb) {
                     if (!wait_or_abort(&full[s], ph, abort_flag)) { give_up(p.status, abort_flag, 0x421); ok = false; break; }
                     tc_fence_after();
                     const uint32_t sfa = tmem + kScaleCol + buf * (12 * S::atoms), sfw = sfa + 4 * S::atoms;
@@ -160,7 +204,7 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         mma_fp4_ss<true, NV>(d, ad + 2 * j, wd + 2 * j, idesc_fp4(256, kRows, NV, NV ? 0 : 2 * (j & 1)), sfa + 4 * (NV ? j : j / 2),
-                                             sfw + 8 * (NV ? j : j / 2), (kb | j) ? 1u : 0u);
+                                             sfw + 8 * (NV ? j : j / 2), (kb > r.kb0 || j > 0) ? 1u : 0u);
                     tc_commit_pair(&empty[s]);
                     if (++s == kStages) { s = 0; ph ^= 1; }
                 }
@@ -172,20 +216,25 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
         const int q = warp & 3;
         uint8_t* const stage = smem + S::out_off + (warp - 2) * (kStageOut * 2048);
         griddep_wait();                                      // nothing is stored before the preceding kernel has completed
-        const bool failed = __any_sync(0xFFFFFFFFu, p.status && *reinterpret_cast<volatile uint32_t*>(p.status) != 0);
+        // (one answer for all four warps, which meet at barriers below; a warp whose wait ran out goes on through them without working)
+        if (warp == 2) *arrived_last = p.status && *reinterpret_cast<volatile uint32_t*>(p.status) != 0;
+        named_barrier(1, 128);
+        const bool failed = *arrived_last != 0;
+        named_barrier(1, 128);
+        bool ok = true;
         int slot = 0;
         for (int i = 0; i < my_tiles; ++i) {
-            int t0, n0;
-            tile_at(i, t0, n0);
+            const Piece r = piece_at(i);
+            const int t0 = r.t0, n0 = r.n0;
+            const bool part = r.kb1 - r.kb0 < p.kblocks;
+            // (this lane's four columns of sums, 128 rows apart)
+            auto sums_of = [&](int of, int begins) { return reinterpret_cast<float4*>(p.parts) + (((size_t)of * 2 + begins) * 2 + rank) * 8192 + q * 32 + lane; };
             const int tw = t0 + rank * kHalf + q * 32, t = tw + lane;      // the warp's first token, this lane's
             const float ar = p.a_rows && t < p.M ? __ldg(p.a_rows + t) : 1.f;
-            if (!warp_wait(d_full, (uint32_t)(i & 1), abort_flag)) { give_up(p.status, abort_flag, 0x430); break; }
-            tc_fence_after();
             const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (i & 1) * kSecond;
             // 32 outputs of 32 tokens, columns c .. c + 31 of the tile
-            auto put = [&](const uint32_t (&v)[32], int c) {
+            auto write = [&](const uint32_t (&v)[32], int c) {
                 const int n = n0 + c;
-                if (tw >= p.M || n >= p.N || failed) return;
                 uint32_t w[16];
                 if (p.w_rows) {
                     if (n + 32 <= p.N && (reinterpret_cast<uintptr_t>(p.w_rows) & 15) == 0) {
@@ -209,7 +258,7 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
                 uint8_t* const buf = stage + slot * 2048;
                 slot = (slot + 1) % kStageOut;
                 if (p.bulk) {
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kStageOut - 1) : "memory");      // the store that last left this buffer
+                    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kStageOut - 1) : "memory");      // the store that last left this buffer
                     __syncwarp();
                 }
 #pragma unroll
@@ -219,9 +268,9 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
                 if (p.bulk && (n + 32 <= p.N || p.N % 8 == 0)) {
                     fence_proxy_async();
                     __syncwarp();
-                    if (lane == 0) tma_store_2d(&maps.out, buf, n, tw);
+                    tma_store_2d_if(lane == 0, &maps.out, buf, n, tw);
                 } else {
-                    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");      // (an empty one: buffers are counted by groups)
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");      // (an empty one: buffers are counted by groups)
                     __syncwarp();
                     const int rows = min(32, p.M - tw);
                     if (n + lane < p.N)
@@ -231,28 +280,141 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
                     __syncwarp();
                 }
             };
-            const int first = (i & 1) ? 0 : kRows - kShared;         // the shared columns come first
-            {
-                uint32_t v[3][32];
+            // the sums of 32 columns from c on: to the workspace, or back, added
+            auto leave = [&](const uint32_t (&v)[32], int c) {
+                float4* const to = sums_of(pair, r.kb0 == 0) + (c >> 2) * 128;
 #pragma unroll
-                for (int c = 0; c < 3; ++c) tmem_ld_32x32(at + first + 32 * c, v[c]);
-                tc_wait_ld();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_pair(issuer(acc_free));
+                for (int j = 0; j < 8; ++j)
+                    __stcg(to + j * 128, make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])));
+            };
+            auto fetch = [&](float4 (&u)[8], int of, int begins, int c) {
+                const float4* at = sums_of(of, begins) + (c >> 2) * 128;
 #pragma unroll
-                for (int c = 0; c < 3; ++c) put(v[c], first + 32 * c);
+                for (int j = 0; j < 8; ++j) u[j] = __ldcg(at + j * 128);
+            };
+            auto add = [&](uint32_t (&v)[32], const float4 (&u)[8]) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + u[j].x);
+                    v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + u[j].y);
+                    v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + u[j].z);
+                    v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + u[j].w);
+                }
+            };
+            // A part: the pairs that have parts of this tile (of k-block u of the cut tiles it is ((u + 1) pairs - 1) / (their k-blocks))
+            int from = 0, to = 0;
+            const int other_begins = r.kb0 != 0;
+            if (part) {
+                const int64_t begin = (int64_t)r.rest_tile * p.kblocks;
+                from = (int)(((begin + 1) * pairs - 1) / rest);
+                to = (int)(((begin + p.kblocks) * pairs - 1) / rest);
             }
-            const int rest = (i & 1) ? kShared : 0;
+            const int byte = from * 2 + rank, shift = 8 * (byte & 3), other = from == pair ? to : from;
+            auto live = [&](int c) { return tw < p.M && n0 + c < p.N && !failed; };
+            if (ok && !warp_wait(d_full, (uint32_t)(i & 1), abort_flag)) { give_up(p.status, abort_flag, 0x430); ok = false; }
+            tc_fence_after();
+            // This CTA arrives at the cut tile: whether it is the last to, and nobody else will look at the counter (all four warps get the answer).
+            auto arrive = [&](bool only_last) -> bool {
+                if (warp == 2) {
+                    uint32_t before = 0u;
+                    if (only_last) before = __shfl_sync(0xFFFFFFFFu, *reinterpret_cast<volatile uint32_t*>(p.counters + (byte >> 2)), 0);
+                    else before = __shfl_sync(0xFFFFFFFFu, atomic_add_if(lane == 0, p.counters + (byte >> 2), 1u << shift), 0);
+                    const bool last = (int)((before >> shift) & 0xFFu) == to - from;
+                    atomic_add_if(last && lane == 0, p.counters + (byte >> 2), 0u - ((uint32_t)(to - from + (only_last ? 0 : 1)) << shift));
+                    *arrived_last = last;
+                }
+                named_barrier(1, 128);
+                const bool last = *arrived_last != 0;
+                if (last) __threadfence();
+                named_barrier(1, 128);
+                return last;
+            };
+            if (part && !failed && to - from == 1 && i == my_tiles - 1) {
+                // the pair's last piece, and one other has the rest of the tile: the accumulators stay where they are, and if the other's sums are there
+                // they come through the shared memory of the stages, which nobody needs any more (a + b is b + a)
+                bool last = arrive(true);
+                if (!last) {
 #pragma unroll 1
-            for (int c = 0; c < kRows - kShared; c += 32) {
-                uint32_t v[32];
-                tmem_ld_32x32(at + rest + c, v);
-                tc_wait_ld();
-                put(v, rest + c);
+                    for (int c = 0; c < kRows; c += 32) {
+                        uint32_t v[32];
+                        if (ok) { tmem_ld_32x32(at + c, v); tc_wait_ld(); }
+                        if (ok && live(c)) leave(v, c);
+                    }
+                    __threadfence();
+                    named_barrier(1, 128);
+                    last = arrive(false);
+                }
+                if (last) {
+                    asm volatile("fence.proxy.async;" ::: "memory");      // (the sums were written by ordinary stores)
+                    if (warp == 2 && elect_one()) {
+                        mbar_expect_tx(sums_full, kHalf * kRows * 4);
+                        tma_bulk_g2s(smem, sums_of(other, other_begins) - (q * 32 + lane), kHalf * kRows * 4, sums_full);
+                    }
+                    __syncwarp();
+                    if (ok && !warp_wait(sums_full, 0u, abort_flag)) { give_up(p.status, abort_flag, 0x431); ok = false; }
+#pragma unroll 1
+                    for (int c = 0; c < kRows; c += 32) {
+                        uint32_t v[32];
+                        if (ok) { tmem_ld_32x32(at + c, v); tc_wait_ld(); }
+                        if (!ok || !live(c)) continue;
+                        float4 u[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) u[j] = reinterpret_cast<const float4*>(smem)[((c >> 2) + j) * 128 + q * 32 + lane];
+                        add(v, u);
+                        write(v, c);
+                    }
+                }
+                break;
+            }
+            if (ok) {
+                auto out = [&](const uint32_t (&v)[32], int c) {
+                    if (!live(c)) return;
+                    if (part) leave(v, c);
+                    else write(v, c);
+                };
+                // the columns that the accumulators share come first
+                const int first = (i & 1) ? 0 : kRows - kShared, behind = (i & 1) ? kShared : 0;
+                {
+                    uint32_t v[3][32];
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) tmem_ld_32x32(at + first + 32 * j, v[j]);
+                    tc_wait_ld();
+                    tc_fence_before();
+                    __syncwarp();
+                    mbar_arrive_pair_if(lane == 0, issuer(acc_free));
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) out(v[j], first + 32 * j);
+                }
+#pragma unroll 1
+                for (int c = behind; c < behind + kRows - kShared; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld_32x32(at + c, v);
+                    tc_wait_ld();
+                    out(v, c);
+                }
+            }
+            if (part && !failed) {
+                __threadfence();
+                named_barrier(1, 128);
+                if (arrive(false)) {
+                    // (more than two parts, or a pair was quicker with its second piece than the other with its last)
+#pragma unroll 1
+                    for (int c = 0; c < kRows; c += 32) {
+                        if (!ok || !live(c)) break;
+                        uint32_t v[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0u;
+                        for (int of = from; of <= to; ++of) {
+                            float4 u[8];
+                            fetch(u, of, of == from, c);
+                            add(v, u);
+                        }
+                        write(v, c);
+                    }
+                }
             }
         }
-        if (lane == 0) bulk_wait_all();
+        bulk_wait_all();
         __syncwarp();
     }
     tc_fence_before();
@@ -298,8 +460,12 @@ static int launch_pair(const Fp4GemmArgs& a, cudaStream_t stream) {
     }
     const int pairs = resident_clusters((const void*)fp4_pair_kernel<NV>, 2, kThreads, S::total);
     if (pairs < 1) return cuda_fail(cudaErrorInvalidConfiguration);
+    Fp4PairPlan plan = fp4_pair_plan(a.M, a.K, a.N, pairs, true);
+    if (fp4_part_bytes(plan) > a.part_bytes) plan = fp4_pair_plan(a.M, a.K, a.N, pairs, false);      // (on a device that holds fewer pairs)
+    p.whole = plan.whole; p.cut = plan.cut;
+    p.counters = a.status + kLrCounterWord; p.parts = a.parts;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(2u * (unsigned)std::min(p.tok_tiles * p.row_tiles, pairs), 1, 1);
+    cfg.gridDim = dim3(2u * (unsigned)plan.pairs, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = S::total;
     cfg.stream = stream;

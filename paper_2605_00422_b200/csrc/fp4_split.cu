@@ -275,9 +275,13 @@ static int launch_format(const Fp4GemmArgs& a, cudaStream_t stream) {
     return a.M <= 16 ? launch_split<NV, 16>(a, stream) : a.M <= 32 ? launch_split<NV, 32>(a, stream) : a.M <= 64 ? launch_split<NV, 64>(a, stream)
                                                                                                              : launch_split<NV, 128>(a, stream);
 }
-int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream) {
+static bool in_pairs(int64_t M, int64_t K, int64_t N) {
     static const int force = getenv("FP4_FORCE") ? atoi(getenv("FP4_FORCE")) : 0;
-    if (force ? force == 2 : a.M > 256) return launch_fp4_pair(a, stream);
+    return force ? force == 2 : M > 256;
+}
+size_t fp4_gemm_part_bytes(int64_t M, int64_t K, int64_t N) { return in_pairs(M, K, N) ? fp4_part_bytes(fp4_pair_plan(M, K, N, kFp4Pairs, true)) : 0; }
+int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream) {
+    if (in_pairs(a.M, a.K, a.N)) return launch_fp4_pair(a, stream);
     return a.format == BWLA_FP4_NV ? launch_format<true>(a, stream) : launch_format<false>(a, stream);
 }
 

@@ -238,6 +238,24 @@ inline bool rot_fp4_groups(const RotGeom& g, int* groups) {
     return g.group_off + *groups * (g.group_bytes + rot_fp4_group_bytes(g)) <= kRotMaxSmem;
 }
 
+// ---- product of microscaled operands in CTA pairs (fp4_pair.cu) ----
+constexpr int kFp4Pairs = 74;            // that a device holds, at most
+constexpr size_t kFp4PartBytes = 2 * 128 * 256 * 4;      // the sums of a tile
+// Pairs, whole tiles of each, and whether the rest is cut by k.  Whole rounds are left whole but for the last full one, which is cut with what does not
+// fill a round.  Fewer tiles than pairs: so many pairs that each has four k-blocks and a tile no more than four parts.
+struct Fp4PairPlan { int pairs, whole; bool cut; };
+inline Fp4PairPlan fp4_pair_plan(int64_t M, int64_t K, int64_t N, int device_pairs, bool cut) {
+    const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), kblocks = (K + 255) / 256;
+    int64_t pairs = std::min(device_pairs, kFp4Pairs);
+    Fp4PairPlan r{};
+    if (tiles < pairs) pairs = !cut ? tiles : std::max(tiles, std::min(pairs, std::min(4 * tiles, tiles * kblocks / 4)));
+    r.pairs = (int)pairs;
+    r.whole = (int)(tiles / pairs);
+    if (cut && tiles % pairs != 0 && r.whole < 8) { r.cut = true; r.whole = std::max(0, r.whole - 1); }      // (one round in nine or more: whole tiles)
+    return r;
+}
+inline size_t fp4_part_bytes(const Fp4PairPlan& r) { return r.cut ? (size_t)r.pairs * 2 * kFp4PartBytes : 0; }
+
 // ---- rotation of many tokens on tcgen05 (rot_umma.cu) ----
 constexpr int kRotUmmaSharedBytes = 1792;      // its barriers and small per-CTA state
 struct RotUmmaGeom {
