@@ -24,7 +24,7 @@ namespace bwla {
 
 namespace fp4_pair {
 constexpr int kTok = 256, kRows = 256, kHalf = 128, kBlockK = 256, kThreads = 192, kStages = 5;
-constexpr int kStageOut = 4;                                       // chunks of 32 tokens x 32 outputs on their way, per epilogue warp
+constexpr int kStageOut = 3;                                       // chunks of 32 tokens x 32 outputs on their way, per epilogue warp
 template <bool NV>
 struct Sizes {
     static constexpr int atoms = NV ? 4 : 2;
@@ -32,7 +32,8 @@ struct Sizes {
     static constexpr int sa_bytes = atoms * 512, sw_bytes = 2 * atoms * 512;
     static constexpr int stage = 2 * half_bytes + sa_bytes + sw_bytes;
     static constexpr int out_off = kStages * stage;
-    static constexpr int bars_off = out_off + 4 * kStageOut * 2048;
+    static constexpr int rows_off = out_off + 4 * kStageOut * 2048;      // the tile's weight row scales, a copy for each epilogue warp
+    static constexpr int bars_off = rows_off + 4 * kRows * 4;
     static constexpr int total = bars_off + (2 * kStages + 3) * 8 + 16 + 1024;
     static_assert(kHalf * kRows * 4 <= kStages * stage, "the sums of a part of a tile lie where the stages were");
     static_assert(total <= 232448, "shared memory");
@@ -215,6 +216,7 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
     } else {
         const int q = warp & 3;
         uint8_t* const stage = smem + S::out_off + (warp - 2) * (kStageOut * 2048);
+        float* const w_row = reinterpret_cast<float*>(smem + S::rows_off) + (warp - 2) * kRows;
         griddep_wait();                                      // nothing is stored before the preceding kernel has completed
         // (one answer for all four warps, which meet at barriers below; a warp whose wait ran out goes on through them without working)
         if (warp == 2) *arrived_last = p.status && *reinterpret_cast<volatile uint32_t*>(p.status) != 0;
@@ -231,25 +233,23 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
             auto sums_of = [&](int of, int begins) { return reinterpret_cast<float4*>(p.parts) + (((size_t)of * 2 + begins) * 2 + rank) * 8192 + q * 32 + lane; };
             const int tw = t0 + rank * kHalf + q * 32, t = tw + lane;      // the warp's first token, this lane's
             const float ar = p.a_rows && t < p.M ? __ldg(p.a_rows + t) : 1.f;
+            if (p.w_rows) {                           // (asked for in the epilogue's loop, their latency took most of its time)
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < kRows / 32; ++j) w_row[32 * j + lane] = n0 + 32 * j + lane < p.N ? __ldg(p.w_rows + n0 + 32 * j + lane) : 0.f;
+                __syncwarp();
+            }
             const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (i & 1) * kSecond;
             // 32 outputs of 32 tokens, columns c .. c + 31 of the tile
             auto write = [&](const uint32_t (&v)[32], int c) {
                 const int n = n0 + c;
                 uint32_t w[16];
                 if (p.w_rows) {
-                    if (n + 32 <= p.N && (reinterpret_cast<uintptr_t>(p.w_rows) & 15) == 0) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float4 f = __ldg(reinterpret_cast<const float4*>(p.w_rows + n) + j);
-                            w[2 * j] = cvt_pair(__uint_as_float(v[4 * j]) * ar * f.x, __uint_as_float(v[4 * j + 1]) * ar * f.y);
-                            w[2 * j + 1] = cvt_pair(__uint_as_float(v[4 * j + 2]) * ar * f.z, __uint_as_float(v[4 * j + 3]) * ar * f.w);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float f0 = n + 2 * j < p.N ? __ldg(p.w_rows + n + 2 * j) : 0.f, f1 = n + 2 * j + 1 < p.N ? __ldg(p.w_rows + n + 2 * j + 1) : 0.f;
-                            w[j] = cvt_pair(__uint_as_float(v[2 * j]) * ar * f0, __uint_as_float(v[2 * j + 1]) * ar * f1);
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        const float4 f = *reinterpret_cast<const float4*>(w_row + c + 4 * j);
+                        w[2 * j] = cvt_pair(__uint_as_float(v[4 * j]) * ar * f.x, __uint_as_float(v[4 * j + 1]) * ar * f.y);
+                        w[2 * j + 1] = cvt_pair(__uint_as_float(v[4 * j + 2]) * ar * f.z, __uint_as_float(v[4 * j + 3]) * ar * f.w);
                     }
                 } else {
 #pragma unroll

@@ -32,7 +32,7 @@ int fp4_operand_maps(CUtensorMap* codes, CUtensorMap* scales, const uint8_t* c, 
 }
 
 namespace fp4_split {
-constexpr int kRows = 128, kBlockK = 256, kThreads = 256, kMaxSplit = 8;
+constexpr int kRows = 128, kBlockK = 256, kThreads = 256;
 template <bool NV, int TOK>
 struct Sizes {
     static constexpr int atoms = NV ? 4 : 2;                     // scale tiles of 4 blocks in a k-block
@@ -192,12 +192,12 @@ __global__ void __launch_bounds__(fp4_split::kThreads, 2) fp4_split_kernel(const
             const float4 f = *reinterpret_cast<const float4*>(red + t * kRows + 4 * lane);
             v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
         } else {
-            uint4 f[kMaxSplit];
+            uint4 f[kFp4MaxSplit];
 #pragma unroll
-            for (int r = 0; r < kMaxSplit; ++r)
+            for (int r = 0; r < kFp4MaxSplit; ++r)
                 if (r < parts) f[r] = ld_shared_cluster_v4(map_shared_rank(mine, (uint32_t)r));
 #pragma unroll
-            for (int r = 0; r < kMaxSplit; ++r)
+            for (int r = 0; r < kFp4MaxSplit; ++r)
                 if (r < parts) {
                     v[0] += __uint_as_float(f[r].x); v[1] += __uint_as_float(f[r].y);
                     v[2] += __uint_as_float(f[r].z); v[3] += __uint_as_float(f[r].w);
@@ -236,15 +236,7 @@ static int launch_split(const Fp4GemmArgs& a, cudaStream_t stream) {
     p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + kBlockK - 1) / kBlockK);
     p.once = tok_tiles == 1; p.a_rows = a.a_rows; p.w_rows = a.w_rows; p.out = a.out; p.ldo = a.ldo; p.status = a.status;
     p.vec = (reinterpret_cast<uintptr_t>(a.out) & 7) == 0 && a.ldo % 4 == 0;
-    // How many CTAs K is cut over.  One an SM leaves room for the kernel behind this one to start beside it (its weights are on their way when
-    // this one ends); more pay where each still has four k-blocks, and up to 13 for 8 SMs clusters of any size fit at once.  In a chain of
-    // calls, us, parts 1 | 2 | 3 | 4 | 5 | 6 | 7 | 8:  5120 x 5120, 1 token 6.6 5.4 5.3 5.1 5.1 5.2 9.1 8.5;  4096 x 4096 5.3 4.5 4.5 4.2 4.5 4.5 5.0 4.9;
-    // 25600 -> 5120, 64 tokens 33 21 17.3 16.1 15.4 15.1 23.4 22.1;  4096 -> 11008, 16 tokens 6.9 6.5 7.0 10.7 ...;  25600 -> 1024, 1 token 23 13.4 10.2
-    // 8.3 7.6 6.8 6.8 6.4.
-    const int64_t sms = std::max(1, sm_count()), tiles = row_tiles * tok_tiles;
-    int64_t cut = std::min<int64_t>(std::min<int64_t>(kMaxSplit, p.kblocks), 13 * sms / 8 / tiles);
-    if (cut * tiles > sms && 4 * cut > p.kblocks) cut = std::max<int64_t>(sms / tiles, p.kblocks / 4);
-    const int parts = (int)std::max<int64_t>(1, cut);
+    const int parts = fp4_split_parts(a.M, a.K, a.N, TOK);
     static thread_local int configured = -1;
     int dev = 0;
     BWLA_CUDA_TRY(cudaGetDevice(&dev));
@@ -275,13 +267,9 @@ static int launch_format(const Fp4GemmArgs& a, cudaStream_t stream) {
     return a.M <= 16 ? launch_split<NV, 16>(a, stream) : a.M <= 32 ? launch_split<NV, 32>(a, stream) : a.M <= 64 ? launch_split<NV, 64>(a, stream)
                                                                                                              : launch_split<NV, 128>(a, stream);
 }
-static bool in_pairs(int64_t M, int64_t K, int64_t N) {
-    static const int force = getenv("FP4_FORCE") ? atoi(getenv("FP4_FORCE")) : 0;
-    return force ? force == 2 : M > 256;
-}
-size_t fp4_gemm_part_bytes(int64_t M, int64_t K, int64_t N) { return in_pairs(M, K, N) ? fp4_part_bytes(fp4_pair_plan(M, K, N, kFp4Pairs, true)) : 0; }
+size_t fp4_gemm_part_bytes(int64_t M, int64_t K, int64_t N) { return fp4_in_pairs(M, K, N) ? fp4_part_bytes(fp4_pair_plan(M, K, N, kFp4Pairs, true)) : 0; }
 int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream) {
-    if (in_pairs(a.M, a.K, a.N)) return launch_fp4_pair(a, stream);
+    if (fp4_in_pairs(a.M, a.K, a.N)) return launch_fp4_pair(a, stream);
     return a.format == BWLA_FP4_NV ? launch_format<true>(a, stream) : launch_format<false>(a, stream);
 }
 

@@ -238,23 +238,47 @@ inline bool rot_fp4_groups(const RotGeom& g, int* groups) {
     return g.group_off + *groups * (g.group_bytes + rot_fp4_group_bytes(g)) <= kRotMaxSmem;
 }
 
-// ---- product of microscaled operands in CTA pairs (fp4_pair.cu) ----
-constexpr int kFp4Pairs = 74;            // that a device holds, at most
-constexpr size_t kFp4PartBytes = 2 * 128 * 256 * 4;      // the sums of a tile
-// Pairs, whole tiles of each, and whether the rest is cut by k.  Whole rounds are left whole but for the last full one, which is cut with what does not
-// fill a round.  Fewer tiles than pairs: so many pairs that each has four k-blocks and a tile no more than four parts.
-struct Fp4PairPlan { int pairs, whole; bool cut; };
-inline Fp4PairPlan fp4_pair_plan(int64_t M, int64_t K, int64_t N, int device_pairs, bool cut) {
-    const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), kblocks = (K + 255) / 256;
-    int64_t pairs = std::min(device_pairs, kFp4Pairs);
+// ---- product of microscaled operands (fp4_split.cu: 128 weight rows x up to 128 tokens a CTA, K cut over a cluster; fp4_pair.cu: 256 x 256 a pair
+//      of CTAs) ----
+constexpr int kFp4Sms = 148, kFp4Pairs = 74;             // what the plans count with; a device that holds fewer takes more rounds
+constexpr int kFp4MaxSplit = 8;
+constexpr size_t kFp4PartBytes = 2 * 128 * 256 * 4;      // the sums of a tile of a pair
+// How many CTAs K is cut over.  One an SM leaves room for the kernel behind this one to start beside it (its weights are on their way when
+// this one ends); more pay where each still has four k-blocks of 256, and up to 13 for 8 SMs clusters of any size fit at once.  In a chain of
+// calls, us, parts 1 | 2 | 3 | 4 | 5 | 6 | 7 | 8:  5120 x 5120, 1 token 6.6 5.4 5.3 5.1 5.1 5.2 9.1 8.5;  4096 x 4096 5.3 4.5 4.5 4.2 4.5 4.5 5.0 4.9;
+// 25600 -> 5120, 64 tokens 33 21 17.3 16.1 15.4 15.1 23.4 22.1;  4096 -> 11008, 16 tokens 6.9 6.5 7.0 10.7 ...;  25600 -> 1024, 1 token 23 13.4 10.2
+// 8.3 7.6 6.8 6.8 6.4.
+inline int fp4_split_parts(int64_t M, int64_t K, int64_t N, int tok) {
+    const int64_t tiles = (N + 127) / 128 * ((M + tok - 1) / tok), kblocks = (K + 255) / 256;
+    int64_t cut = std::min<int64_t>(std::min<int64_t>(kFp4MaxSplit, kblocks), 13 * kFp4Sms / 8 / tiles);
+    if (cut * tiles > kFp4Sms && 4 * cut > kblocks) cut = std::max<int64_t>(kFp4Sms / tiles, kblocks / 4);
+    return (int)std::max<int64_t>(1, cut);
+}
+// Pairs, whole tiles of each, and whether the rest is cut by k: the last full round with what does not fill a round, or tiles in two where there
+// are no more than half as many as pairs.  A cut costs some 10 us (the sums of parts go through the L2), so it has to save more: time in ns.
+struct Fp4PairPlan { int pairs, whole; bool cut; int64_t ns; };
+inline Fp4PairPlan fp4_pair_plan(int64_t M, int64_t K, int64_t N, int device_pairs, bool may_cut) {
+    const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), kblocks = (K + 255) / 256, most = std::min(device_pairs, kFp4Pairs);
+    const int64_t block = 360;
     Fp4PairPlan r{};
-    if (tiles < pairs) pairs = !cut ? tiles : std::max(tiles, std::min(pairs, std::min(4 * tiles, tiles * kblocks / 4)));
-    r.pairs = (int)pairs;
-    r.whole = (int)(tiles / pairs);
-    if (cut && tiles % pairs != 0 && r.whole < 8) { r.cut = true; r.whole = std::max(0, r.whole - 1); }      // (one round in nine or more: whole tiles)
+    r.pairs = (int)std::min(tiles, most);
+    r.whole = (int)(tiles / r.pairs);
+    r.ns = 6000 + (tiles + r.pairs - 1) / r.pairs * kblocks * block;
+    const int64_t pairs = tiles >= most ? most : std::min(most, 2 * tiles);
+    const int64_t ns = 16000 + tiles * kblocks * block / pairs;
+    if (may_cut && tiles % pairs != 0 && kblocks > 1 && ns < r.ns) { r.pairs = (int)pairs; r.whole = std::max(0, (int)(tiles / pairs) - 1); r.cut = true; r.ns = ns; }
     return r;
 }
 inline size_t fp4_part_bytes(const Fp4PairPlan& r) { return r.cut ? (size_t)r.pairs * 2 * kFp4PartBytes : 0; }
+// Which of the two takes a product.  us, fp4_split.cu | fp4_pair.cu (MX; * cut): 257 x 4096 x 4096 (tokens x K x N) 11.4 | 12; 333 x 11008 x 4096 19.3 | 24.5;
+// 512 x 4096 x 4096 11.5 | 11.8; 200 x 25600 x 5120 25.6 | 34 *; 512 x 5120 x 25600 45 | 35; 1024 x 25600 x 5120 104 | 54 *; 2048 x 5120 x 8192 56 | 37; 4096 x 5120 x
+// 25600 318 | 188.
+inline bool fp4_in_pairs(int64_t M, int64_t K, int64_t N) {
+    if (M <= 128) return false;
+    const int64_t tiles = (N + 127) / 128 * ((M + 127) / 128), kblocks = (K + 255) / 256, parts = fp4_split_parts(M, K, N, 128);
+    const int64_t split = 6500 + (tiles * parts + kFp4Sms - 1) / kFp4Sms * ((kblocks + parts - 1) / parts) * 300;
+    return fp4_pair_plan(M, K, N, kFp4Pairs, true).ns < split;
+}
 
 // ---- rotation of many tokens on tcgen05 (rot_umma.cu) ----
 constexpr int kRotUmmaSharedBytes = 1792;      // its barriers and small per-CTA state
