@@ -462,12 +462,29 @@ def bwla_fp4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
     return int(_lib.bwla_fp4_gemm_workspace_bytes(M, K, N))
 
 
+def _fp4_scratch(n: int, device) -> torch.Tensor:
+    ws = torch.empty(max(256, n), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def _fp4_need(t: torch.Tensor, dtype, name: str, ndim: int):
+    _need(t, dtype, name, ndim)
+    if t.device.index != torch.cuda.current_device():
+        raise TypeError(f"{name}: expected a tensor of the current CUDA device")
+
+
+def _fp4_stride(x: torch.Tensor) -> int:
+    """Elements from a row to the next; of a single row, whose stride may be anything, at least its length."""
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0) if x.shape[0] else 0, x.shape[1])
+
+
 def new_fp4_workspace(M: int, K: int, N: int, device="cuda") -> torch.Tensor:
-    """Scratch buffer for bwla_fp4_gemm_codes (zero-filled)."""
+    """Scratch buffer for bwla_fp4_gemm_codes (its status words zero)."""
     n = bwla_fp4_gemm_workspace_bytes(M, K, N)
     if n == 0:
         raise ValueError("invalid dimensions")
-    return torch.zeros(n, dtype=torch.uint8, device=device)
+    return _fp4_scratch(n, device)
 
 
 def bwla_fp4_gemm_codes(a_codes: torch.Tensor, a_scales: torch.Tensor, a_rows: Optional[torch.Tensor], w_codes: torch.Tensor,
@@ -488,16 +505,17 @@ def bwla_rotate_quant_fp4_workspace_bytes(M: int, K: int, n1: int, n2: int) -> i
 
 def bwla_rotate_quant_fp4(x: torch.Tensor, P1: torch.Tensor, P2: torch.Tensor, format: int, workspace: Optional[torch.Tensor] = None):
     """x: bf16 [M][K] -> (codes, scale tiles, row scales or None) of the rows rotated by P1 (x) P2."""
-    _need(x, torch.bfloat16, "x", 2)
-    _need(P1, torch.float32, "P1", 2)
-    _need(P2, torch.float32, "P2", 2)
+    _fp4_need(x, torch.bfloat16, "x", 2)
+    _fp4_need(P1, torch.float32, "P1", 2)
+    _fp4_need(P2, torch.float32, "P2", 2)
     if not (P1.is_contiguous() and P2.is_contiguous()):
         raise TypeError("P1 and P2 must be contiguous")
     M, K = x.shape
     if workspace is None:
-        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, K, P1.shape[0], P2.shape[0])), dtype=torch.uint8, device=x.device)
+        workspace = _fp4_scratch(bwla_rotate_quant_fp4_workspace_bytes(M, K, P1.shape[0], P2.shape[0]), x.device)
+    _fp4_need(workspace, torch.uint8, "workspace", 1)
     codes, scales, rows = _fp4_outputs(M, K, format, x.device)
-    st = _lib.bwla_rotate_quant_fp4(_ptr(x), M, K, x.stride(0) if M > 0 else K, _ptr(P1), P1.shape[0], _ptr(P2), P2.shape[0], format, _ptr(codes),
+    st = _lib.bwla_rotate_quant_fp4(_ptr(x), M, K, _fp4_stride(x), _ptr(P1), P1.shape[0], _ptr(P2), P2.shape[0], format, _ptr(codes),
                                     _ptr(scales), _ptr(rows), _ptr(workspace), workspace.numel(), _stream())
     _check(st, "bwla_rotate_quant_fp4")
     return codes, scales, rows
@@ -507,12 +525,12 @@ class Fp4Layer:
     """A prepared 4-bit layer (bwla_fp4_layer_create): keeps the handle, the tensors it points into and the prepared buffer."""
 
     def __init__(self, P1, P2, format, w_codes, w_scales, w_rows=None):
-        _need(P1, torch.float32, "P1", 2)
-        _need(P2, torch.float32, "P2", 2)
-        _need(w_codes, torch.uint8, "w_codes", 2)
-        _need(w_scales, torch.uint8, "w_scales", 1)
+        _fp4_need(P1, torch.float32, "P1", 2)
+        _fp4_need(P2, torch.float32, "P2", 2)
+        _fp4_need(w_codes, torch.uint8, "w_codes", 2)
+        _fp4_need(w_scales, torch.uint8, "w_scales", 1)
         if w_rows is not None:
-            _need(w_rows, torch.float32, "w_rows", 1)
+            _fp4_need(w_rows, torch.float32, "w_rows", 1)
         if not (w_codes.is_contiguous() and P1.is_contiguous() and P2.is_contiguous()):
             raise TypeError("w_codes, P1 and P2 must be contiguous")
         self.N, self.K, self.format = w_codes.shape[0], 2 * w_codes.shape[1], format
@@ -553,14 +571,15 @@ def bwla_fp4_layer_destroy(layer: Fp4Layer) -> None:
 
 def bwla_fp4_layer_rotate_quant(layer: Fp4Layer, x: torch.Tensor, workspace: Optional[torch.Tensor] = None):
     """x: bf16 [M][K] -> (codes, scale tiles, row scales or None) of the rotated rows, through a prepared layer."""
-    _need(x, torch.bfloat16, "x", 2)
+    _fp4_need(x, torch.bfloat16, "x", 2)
     M = x.shape[0]
     if x.shape[1] != layer.K:
         raise TypeError("x must be [M][K] of the layer")
     if workspace is None:
-        workspace = torch.zeros(max(256, bwla_rotate_quant_fp4_workspace_bytes(M, layer.K, layer.n1, layer.n2)), dtype=torch.uint8, device=x.device)
+        workspace = _fp4_scratch(bwla_rotate_quant_fp4_workspace_bytes(M, layer.K, layer.n1, layer.n2), x.device)
+    _fp4_need(workspace, torch.uint8, "workspace", 1)
     codes, scales, rows = _fp4_outputs(M, layer.K, layer.format, x.device)
-    st = _lib.bwla_fp4_layer_rotate_quant(layer.handle, _ptr(x), M, x.stride(0) if M > 0 else layer.K, _ptr(codes), _ptr(scales), _ptr(rows),
+    st = _lib.bwla_fp4_layer_rotate_quant(layer.handle, _ptr(x), M, _fp4_stride(x), _ptr(codes), _ptr(scales), _ptr(rows),
                                           _ptr(workspace), workspace.numel(), _stream())
     _check(st, "bwla_fp4_layer_rotate_quant")
     return codes, scales, rows
@@ -571,8 +590,8 @@ def bwla_fp4_layer_workspace_bytes(layer: Fp4Layer, M: int) -> int:
 
 
 def new_fp4_layer_workspace(layer: Fp4Layer, M: int, device="cuda") -> torch.Tensor:
-    """Scratch buffer for bwla_fp4_layer_linear (zero-filled)."""
-    return torch.zeros(max(256, bwla_fp4_layer_workspace_bytes(layer, M)), dtype=torch.uint8, device=device)
+    """Scratch buffer for bwla_fp4_layer_linear (its status words zero)."""
+    return _fp4_scratch(bwla_fp4_layer_workspace_bytes(layer, M), device)
 
 
 def bwla_fp4_layer_linear(layer: Fp4Layer, x: torch.Tensor, out: Optional[torch.Tensor] = None,

@@ -275,6 +275,7 @@ inline size_t fp4_part_bytes(const Fp4PairPlan& r) { return r.cut ? (size_t)r.pa
 // 25600 318 | 188.
 inline bool fp4_in_pairs(int64_t M, int64_t K, int64_t N) {
     if (M <= 128) return false;
+    if ((M + 127) / 128 > 65535) return true;            // (what a grid's second dimension holds)
     const int64_t tiles = (N + 127) / 128 * ((M + 127) / 128), kblocks = (K + 255) / 256, parts = fp4_split_parts(M, K, N, 128);
     const int64_t split = 6500 + (tiles * parts + kFp4Sms - 1) / kFp4Sms * ((kblocks + parts - 1) / parts) * 300;
     return fp4_pair_plan(M, K, N, kFp4Pairs, true).ns < split;

@@ -5,6 +5,8 @@
 // whichever build of the library the process has loaded is the one that is called.  As through ctypes, other threads run while the
 // library works, and what PyTorch throws (a tensor without memory of its own, a stream of a device that is not there) becomes a Python
 // exception.
+#include <algorithm>
+
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -194,6 +196,15 @@ bool here(const at::Tensor& t, const char* name) {
     PyErr_Format(PyExc_TypeError, "%s: expected a tensor of the current CUDA device", name);
     return false;
 }
+// Elements from a row to the next; of a single row, whose stride may be anything, at least its length.
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : std::max(t.size(0) == 1 ? t.stride(0) : 0, t.size(1)); }
+// A workspace: one piece of memory of the current device.
+const at::Tensor* workspace(PyObject* o) {
+    const at::Tensor* t = tensor(o, "workspace");
+    if (!t || !here(*t, "workspace")) return nullptr;
+    if (!t->is_contiguous()) { PyErr_SetString(PyExc_TypeError, "workspace: expected a contiguous tensor"); return nullptr; }
+    return t;
+}
 // tensors that are long enough for their rows: the library sees pointers only
 bool fp4_rows(PyObject* codes, PyObject* scales, PyObject* row_scales, int format, const char* names[3], Fp4Rows* out) {
     const at::Tensor *c = need(codes, at::kByte, names[0], 2), *s, *r = nullptr;
@@ -247,7 +258,7 @@ PyObject* call_fp4_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
     const Ref rows = args[4] != Py_None || format != BWLA_FP4_NV ? Ref(Py_NewRef(args[4])) : fp4_new({M}, at::kFloat, *x);
     if (!codes.o || !scales.o || !rows.o || !fp4_rows(codes.o, scales.o, rows.o, format, names, &q)) return nullptr;
     if (q.rows != M || q.K != K / 2 * 2) { PyErr_SetString(PyExc_TypeError, "codes must be [M][K/2] for x of [M][K]"); return nullptr; }
-    return fp4_result(unlocked(entry.fp4_quantize, (const void*)x->data_ptr(), float_dtype(*x), M, K, M > 0 ? x->stride(0) : K, format, (uint8_t*)q.codes,
+    return fp4_result(unlocked(entry.fp4_quantize, (const void*)x->data_ptr(), float_dtype(*x), M, K, row_stride(*x), format, (uint8_t*)q.codes,
                                (uint8_t*)q.scales, (float*)q.row_scales, stream()),
                       PyTuple_Pack(3, codes.o, scales.o, rows.o));
     END_HANDLE_TH_ERRORS
@@ -268,7 +279,7 @@ PyObject* call_fp4_expand(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!need(made.o, out->scalar_type(), "out", 2) || !here(*out, "out")) return nullptr;
     if (out->size(0) != q.rows || out->size(1) != q.K) { PyErr_SetString(PyExc_TypeError, "out must be [M][K] for codes of [M][K/2]"); return nullptr; }
     return fp4_result(unlocked(entry.fp4_expand, (const uint8_t*)q.codes, (const uint8_t*)q.scales, (const float*)q.row_scales, q.rows, q.K, format,
-                               out->data_ptr(), float_dtype(*out), q.rows > 0 ? out->stride(0) : q.K, stream()),
+                               out->data_ptr(), float_dtype(*out), row_stride(*out), stream()),
                       Py_NewRef(made.o));
     END_HANDLE_TH_ERRORS
 }
@@ -284,14 +295,14 @@ PyObject* call_fp4_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!fp4_format(args[6], &format) || !fp4_rows(args[0], args[1], args[2], format, a_names, &a) || !fp4_rows(args[3], args[4], args[5], format, w_names, &w))
         return nullptr;
     const Ref made = args[7] != Py_None ? Ref(Py_NewRef(args[7])) : fp4_new({a.rows, w.rows}, at::kBFloat16, THPVariable_Unpack(args[0]));
-    if (!made.o || !(out = need(made.o, at::kBFloat16, "out", 2)) || !here(*out, "out") || !(ws = tensor(args[8], "workspace")) || !here(*ws, "workspace"))
+    if (!made.o || !(out = need(made.o, at::kBFloat16, "out", 2)) || !here(*out, "out") || !(ws = workspace(args[8])))
         return nullptr;
     if (a.K != w.K || out->size(0) != a.rows || out->size(1) != w.rows) {
         PyErr_SetString(PyExc_TypeError, "a_codes [M][K/2], w_codes [N][K/2] and out [M][N] do not fit");
         return nullptr;
     }
     return fp4_result(unlocked(entry.fp4_gemm, (const uint8_t*)a.codes, (const uint8_t*)a.scales, (const float*)a.row_scales, a.rows, a.K, (const uint8_t*)w.codes,
-                               (const uint8_t*)w.scales, (const float*)w.row_scales, w.rows, format, out->data_ptr(), a.rows > 0 ? out->stride(0) : w.rows,
+                               (const uint8_t*)w.scales, (const float*)w.row_scales, w.rows, format, out->data_ptr(), row_stride(*out),
                                ws->data_ptr(), (size_t)ws->nbytes(), stream()),
                       Py_NewRef(made.o));
     END_HANDLE_TH_ERRORS
@@ -302,7 +313,7 @@ PyObject* call_fp4_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
     if (nargs != 4) { PyErr_SetString(PyExc_TypeError, "fp4_linear(layer, x, out, workspace)"); return nullptr; }
     const at::Tensor *x = need(args[1], at::kBFloat16, "x", 2), *out, *ws;
-    if (!x || !here(*x, "x") || !(ws = tensor(args[3], "workspace")) || !here(*ws, "workspace")) return nullptr;
+    if (!x || !here(*x, "x") || !(ws = workspace(args[3]))) return nullptr;
     const Ref h(PyObject_GetAttr(args[0], name_fp4));
     if (!h.o) return nullptr;
     const bwla_fp4_layer* layer = h.o == Py_None ? nullptr : (const bwla_fp4_layer*)PyLong_AsVoidPtr(h.o);
@@ -312,7 +323,7 @@ PyObject* call_fp4_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const Ref made = args[2] != Py_None ? Ref(Py_NewRef(args[2])) : fp4_new({M, N}, at::kBFloat16, *x);
     if (!made.o || !(out = need(made.o, at::kBFloat16, "out", 2)) || !here(*out, "out")) return nullptr;
     if (x->size(1) != K || out->size(0) != M || out->size(1) != N) { PyErr_SetString(PyExc_TypeError, "x must be [M][K] and out [M][N] of the layer"); return nullptr; }
-    return fp4_result(unlocked(entry.fp4_linear, layer, (const void*)x->data_ptr(), M, M > 0 ? x->stride(0) : K, out->data_ptr(), M > 0 ? out->stride(0) : N,
+    return fp4_result(unlocked(entry.fp4_linear, layer, (const void*)x->data_ptr(), M, row_stride(*x), out->data_ptr(), row_stride(*out),
                                ws->data_ptr(), (size_t)ws->nbytes(), stream()),
                       Py_NewRef(made.o));
     END_HANDLE_TH_ERRORS

@@ -445,3 +445,120 @@ def test_a_failed_workspace_keeps_its_word(bwla):
     assert bwla.bwla_check_status(ws) == bwla.BWLA_ERR_DEVICE_TIMEOUT
     check_product(bwla.bwla_fp4_gemm_codes(a, sa, None, w, sw, None, 0, workspace=ws), va, vw, exact=True)
     assert bwla.bwla_check_status(ws) == 0
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 256, 512), (700, 1024, 1024), (1100, 5120, 25600)])
+def test_a_failed_workspace_keeps_its_word_whatever_the_kernel(bwla, M, N, K):
+    """The same for the kernels of many tokens, cut tiles among them: no output is written, and after the check the call is right."""
+    rng = np.random.default_rng(M)
+    a, sa, va = operand(rng, M, K, "nv", integers=True)
+    w, sw, vw = operand(rng, N, K, "nv", integers=True)
+    ws = bwla.new_fp4_workspace(M, K, N)
+    ws[:4].view(torch.int32)[0] = 1
+    out = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    bwla.bwla_fp4_gemm_codes(a, sa, None, w, sw, None, 1, out=out, workspace=ws)
+    assert bwla.bwla_check_status(ws) == bwla.BWLA_ERR_DEVICE_TIMEOUT and (out == 7).all()
+    check_product(bwla.bwla_fp4_gemm_codes(a, sa, None, w, sw, None, 1, out=out, workspace=ws), va, vw, exact=True)
+    assert bwla.bwla_check_status(ws) == 0 and not ws[:256].any()      # (arrival counters are back at zero)
+
+
+# tiles of 256 x 256 in one round and a half, in fewer halves than pairs, cut in three; more than one round of whole tiles
+CUT = [(1024, 5120, 25600), (1000, 1000, 32000), (250, 1030, 25600), (500, 3333, 20480), (2048, 2600, 12800), (1300, 4096, 8192), (2304, 2304, 512)]
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K", CUT)
+def test_product_of_tiles_cut_by_k(bwla, fmt, M, N, K):
+    rng = np.random.default_rng([M, N, K, 3])
+    a, sa, va = operand(rng, M, K, fmt)
+    w, sw, vw = operand(rng, N, K, fmt)
+    ra, rw = torch.rand(M, device="cuda") + 0.5, torch.rand(N, device="cuda") - 0.5
+    ws = bwla.new_fp4_workspace(M, K, N)
+    ws[256:].fill_(255)                              # what was in the scratch before is not looked at
+    out = bwla.bwla_fp4_gemm_codes(a, sa, ra, w, sw, rw, FORMATS[fmt], workspace=ws)
+    assert bwla.bwla_check_status(ws) == 0 and not ws[:256].any()
+    check_product(out, va, vw, ra, rw)
+    for _ in range(5):
+        assert torch.equal(bwla.bwla_fp4_gemm_codes(a, sa, ra, w, sw, rw, FORMATS[fmt], workspace=ws), out)
+
+
+@pytest.mark.parametrize("M", [1, 20, 130, 600])
+@pytest.mark.parametrize("shift", [1, 2, 4, 8])
+def test_outputs_off_16_bytes(bwla, M, shift):
+    """The output begins anywhere on 2 bytes inside its rows; what is beside it stays."""
+    rng = np.random.default_rng([M, shift])
+    N, K = 520, 1024
+    a, sa, va = operand(rng, M, K, "mx", integers=True)
+    w, sw, vw = operand(rng, N, K, "mx", integers=True)
+    wide = torch.full((M, N + 24), 7.0, dtype=torch.bfloat16, device="cuda")
+    bwla.bwla_fp4_gemm_codes(a, sa, None, w, sw, None, 0, out=wide[:, shift:N + shift])
+    check_product(wide[:, shift:N + shift], va, vw, exact=True)
+    assert (wide[:, :shift] == 7).all() and (wide[:, N + shift:] == 7).all()
+
+
+def test_a_single_row_of_any_stride(bwla):
+    K, N = 96, 64
+    x = torch.randn(K, 1, device="cuda").t()         # [1][K], row stride 1
+    assert x.stride(0) == 1
+    q = bwla.bwla_fp4_quantize_rows(x, 1)
+    want = bwla.bwla_fp4_quantize_rows(x.clone(memory_format=torch.contiguous_format), 1)
+    assert torch.equal(bwla.bwla_fp4_expand_rows(*q, 1), bwla.bwla_fp4_expand_rows(*want, 1))       # (scale bytes of rows beyond the last may differ)
+    w = bwla.bwla_fp4_quantize_rows(torch.randn(N, K, device="cuda"), 1)
+    out = torch.empty(N, 1, dtype=torch.bfloat16, device="cuda").t()
+    assert torch.equal(bwla.bwla_fp4_gemm_codes(*q, *w, 1, out=out), bwla.bwla_fp4_gemm_codes(*want, *w, 1))
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("n1,n2,M", [(64, 64, 3), (64, 64, 500), (86, 128, 9), (64, 128, 400)])
+def test_rotation_of_rows_off_16_bytes(bwla, fmt, n1, n2, M):
+    rng = np.random.default_rng([n1, n2, M, 8])
+    K = n1 * n2
+    big = dev(rng.standard_normal((M, K + 3))).bfloat16()
+    x = big[:, 1:K + 1]
+    P1, P2 = haar(rng, n1), haar(rng, n2)
+    check_rotated(bwla, x, P1, P2, fmt, bwla.bwla_rotate_quant_fp4(x, dev(P1), dev(P2), FORMATS[fmt]))
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_other_streams(bwla, fmt):
+    """Calls on two streams at once, with workspaces of their own."""
+    K, N = 4096, 1024
+    w = bwla.bwla_fp4_quantize_rows(torch.randn(N, K, device="cuda"), FORMATS[fmt])
+    P1, P2 = dev(haar(np.random.default_rng(0), 64)), dev(haar(np.random.default_rng(1), 64))
+    layer = bwla.bwla_fp4_layer_create(P1, P2, FORMATS[fmt], *w)
+    xs = [torch.randn(M, K, device="cuda").bfloat16() for M in (5, 300)]
+    want = [bwla.bwla_fp4_layer_linear(layer, x) for x in xs]
+    wss = [bwla.new_fp4_layer_workspace(layer, x.shape[0]) for x in xs]
+    outs = [torch.empty_like(y) for y in want]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, x, o, ws in zip(streams, xs, outs, wss):
+            with torch.cuda.stream(s):
+                bwla.bwla_fp4_layer_linear(layer, x, out=o, workspace=ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, y) for o, y in zip(outs, want))
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("n1,n2", [(64, 64), (86, 128), (64, 88)])
+def test_rotated_weights_without_a_synchronisation(bwla, fmt, n1, n2):
+    """Weights that the kernel before makes (rotation and quantiser), read by the product at once."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    K, N, M = n1 * n2, 384, 16
+    P1, P2 = dev(haar(np.random.default_rng(0), n1)), dev(haar(np.random.default_rng(1), n2))
+    Ws = [torch.randn(N, K, device="cuda", generator=g).bfloat16() for _ in range(4)]
+    a = bwla.bwla_fp4_quantize_rows(torch.randn(M, K, device="cuda", generator=g), FORMATS[fmt])
+    ws, ws2 = bwla.new_fp4_workspace(M, K, N), bwla._fp4_scratch(bwla.bwla_rotate_quant_fp4_workspace_bytes(N, K, n1, n2), "cuda")
+    want = []
+    for W in Ws:
+        q = bwla.bwla_rotate_quant_fp4(W, P1, P2, FORMATS[fmt])
+        torch.cuda.synchronize()
+        want.append(bwla.bwla_fp4_gemm_codes(*a, *q, FORMATS[fmt], workspace=ws))
+        torch.cuda.synchronize()
+        del q
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [bwla.bwla_fp4_gemm_codes(*a, *bwla.bwla_rotate_quant_fp4(W, P1, P2, FORMATS[fmt], workspace=ws2), FORMATS[fmt], workspace=ws) for W in Ws]
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(got, want))
