@@ -86,7 +86,7 @@ def build_calls(force: bool = False) -> str:
            sysconfig.get_paths()["include"], "/usr/local/cuda/include"]
     lib = os.path.join(troot, "lib")
     cmd = (["g++", "-std=c++17", "-O2", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
-           [f"-I{d}" for d in inc] + ["-o", CALLS, src, f"-L{lib}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+           [f"-I{d}" for d in inc] + ["-o", CALLS, src, f"-L{lib}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
                                       f"-Wl,-rpath,{lib}"])
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:

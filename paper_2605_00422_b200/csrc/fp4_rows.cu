@@ -21,10 +21,17 @@ constexpr int kPiece = 16;                // values
 
 template <typename T> struct RawPiece { uint4 v[sizeof(T)]; };      // 32 or 64 bytes
 
+// vec: bytes that rows are aligned to, 32 or 16, or 0
 template <typename T>
-__device__ __forceinline__ RawPiece<T> load_piece(const T* p, bool vec) {
+__device__ __forceinline__ RawPiece<T> load_piece(const T* p, int vec) {
     RawPiece<T> r;
-    if (vec) {
+    if (vec == 32) {                      // (whole sectors a lane)
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); i += 2)
+            asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w), "=r"(r.v[i + 1].x), "=r"(r.v[i + 1].y), "=r"(r.v[i + 1].z), "=r"(r.v[i + 1].w)
+                         : "l"(reinterpret_cast<const uint4*>(p) + i));
+    } else if (vec) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T); ++i) r.v[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
     } else {
@@ -96,7 +103,7 @@ template <typename T, bool NV, int P, int ROWS>
 __global__ void __launch_bounds__(ROWS > 1 ? 32 * ROWS : 1024) fp4_quantize_kernel(const Fp4QuantParams p) {
     __shared__ uint32_t red[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int tid = ROWS > 1 ? lane : (int)(NV ? threadIdx.x : blockIdx.y * blockDim.x + threadIdx.x), G = ROWS > 1 ? 32 : (int)blockDim.x;
+    const int tid = ROWS > 1 ? lane : (int)(NV ? threadIdx.x : blockIdx.y * (P > 0 ? P : 1) * blockDim.x + threadIdx.x), G = ROWS > 1 ? 32 : (int)blockDim.x;
     const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? warp : 0);
     const bool live = row < p.M;
     const int pieces = (int)(p.K >> 4);
@@ -104,7 +111,7 @@ __global__ void __launch_bounds__(ROWS > 1 ? 32 * ROWS : 1024) fp4_quantize_kern
     const T* x = reinterpret_cast<const T*>(p.x) + (live ? row : 0) * p.ldx;
     uint2* const codes = reinterpret_cast<uint2*>(p.codes) + row * pieces;
     uint8_t* const scales = p.scales + fp4_scale_at(row, 0, p.col_tiles);
-    const bool vec = p.vec != 0;
+    const int vec = p.vec;
     griddep_wait();
     if (p.chained) griddep_launch_dependents();
     auto load = [&](int c) {
@@ -171,7 +178,7 @@ __global__ void __launch_bounds__(ROWS > 1 ? 32 * ROWS : 1024) fp4_quantize_kern
     if (P > 0) {
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            if (i * G < full) put(tid + i * G, held[i]);
+            if (tid - (int)(ROWS > 1 ? lane : threadIdx.x) + i * G < full) put(tid + i * G, held[i]);
     } else {
         for (int c = tid; c - tid < full; c += G) put(c, load(c));
     }
@@ -190,12 +197,12 @@ static int quantize_rows(const Fp4QuantParams& p, cudaStream_t stream) {
         rows = 8; threads = 256;
         k = full <= 32 ? fp4_quantize_kernel<T, NV, 1, 8> : fp4_quantize_kernel<T, NV, 2, 8>;
     } else {
-        // (blocks of MX are independent: a row in parts)
-        const int per = !NV || full <= 512 ? 1 : full <= 1024 ? 2 : full <= 1024 * kMost ? kMost : 0;
-        if (!NV) parts = (full + 511) / 512;
+        // 64 bytes a thread in flight where the row is long enough (blocks of MX are independent: a row in parts)
+        constexpr int kFew = sizeof(T) == 4 ? 1 : 2;
+        if (!NV) parts = (full + 512 * kFew - 1) / (512 * kFew);
+        const int per = !NV || full <= 512 * kFew ? kFew : full <= 1024 * kMost ? kMost : 0;
         if (per) threads = (int)((full + 32 * per * parts - 1) / (32 * per * parts) * 32);
-        k = !NV ? fp4_quantize_kernel<T, NV, 1, 1> : per == 1 ? fp4_quantize_kernel<T, NV, 1, 1> : per == 2 ? fp4_quantize_kernel<T, NV, NV ? 2 : 1, 1> : per ? fp4_quantize_kernel<T, NV, NV ? kMost : 1, 1>
-                                                                                               : fp4_quantize_kernel<T, NV, NV ? 0 : 1, 1>;
+        k = per == kFew ? fp4_quantize_kernel<T, NV, kFew, 1> : per ? fp4_quantize_kernel<T, NV, NV ? kMost : kFew, 1> : fp4_quantize_kernel<T, NV, NV ? 0 : kFew, 1>;
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((p.M + rows - 1) / rows), (unsigned)parts, 1);
@@ -218,7 +225,8 @@ int launch_fp4_quantize(const void* x, int dtype, int64_t M, int64_t K, int64_t 
     p.x = x; p.M = M; p.K = K; p.ldx = ldx; p.codes = codes; p.scales = scales; p.row_scales = row_scales;
     p.chained = chained;
     p.col_tiles = fp4_col_tiles(K, format);
-    p.vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && ldx % (dtype == BWLA_DTYPE_F32 ? 4 : 8) == 0;
+    const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(x) & 31) | (ldx * (dtype == BWLA_DTYPE_F32 ? 4 : 2)) % 32;      // (of any row from 32 bytes)
+    p.vec = off == 0 ? 32 : off % 16 == 0 ? 16 : 0;
     const bool nv = format == BWLA_FP4_NV;
     if (dtype == BWLA_DTYPE_F32) return nv ? quantize_rows<float, true>(p, stream) : quantize_rows<float, false>(p, stream);
     if (dtype == BWLA_DTYPE_BF16) return nv ? quantize_rows<__nv_bfloat16, true>(p, stream) : quantize_rows<__nv_bfloat16, false>(p, stream);
@@ -264,28 +272,28 @@ __device__ __forceinline__ void expand_piece(T* out, uint32_t codes, uint32_t by
     }
 }
 
-// A thread takes two pieces of 8 values, ROWS rows a block a warp each (short rows), or a part of one row a block; rows beyond the grid's second
+// A thread takes U pieces of 8 values, ROWS rows a block a warp each (short rows), or a part of one row a block; rows beyond the grid's second
 // dimension in turn.
-template <typename T, bool NV, int ROWS>
+template <typename T, bool NV, int ROWS, int U>
 __global__ void __launch_bounds__(ROWS > 1 ? 32 * ROWS : 512) fp4_expand_kernel(const Fp4ExpandParams p) {
     const int pieces = (int)(p.K >> 3);
     const int step = ROWS > 1 ? 32 : (int)blockDim.x;
-    const int c0 = ROWS > 1 ? (int)(threadIdx.x & 31) : (int)(blockIdx.x * 2 * blockDim.x + threadIdx.x);
+    const int c0 = ROWS > 1 ? (int)(threadIdx.x & 31) : (int)(blockIdx.x * U * blockDim.x + threadIdx.x);
     griddep_wait();
     for (int64_t row = (int64_t)blockIdx.y * ROWS + (ROWS > 1 ? threadIdx.x >> 5 : 0); row < p.M; row += (int64_t)gridDim.y * ROWS) {
         const uint32_t* codes = reinterpret_cast<const uint32_t*>(p.codes) + row * pieces;
         const uint8_t* scales = p.scales + fp4_scale_at(row, 0, p.col_tiles);
         const float r = p.row_scales ? __ldg(p.row_scales + row) : 1.f;
         T* out = reinterpret_cast<T*>(p.out) + (size_t)row * p.ldo;
-        uint32_t word[2], byte[2];
+        uint32_t word[U], byte[U];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int c = c0 + u * step, j = c >> (NV ? 1 : 2);
             word[u] = c < pieces ? __ldg(codes + c) : 0u;
             byte[u] = c < pieces ? __ldg(scales + (size_t)(j >> 2) * 512 + (j & 3)) : 0u;
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int c = c0 + u * step;
             if (c < pieces) expand_piece<T, NV>(out + (size_t)c * 8, word[u], byte[u], r, p.vec != 0);
         }
@@ -296,8 +304,9 @@ template <typename T, bool NV>
 static int expand_rows(const Fp4ExpandParams& p, cudaStream_t stream) {
     const int64_t pieces = p.K / 8;
     const bool several = pieces <= 64;
-    const int64_t parts = (pieces + 1023) / 1024;
-    const int threads = several ? 256 : (int)(((pieces + 2 * parts - 1) / (2 * parts) + 31) / 32 * 32);
+    constexpr int U = sizeof(T) == 4 ? 2 : 4;                   // (64 bytes of stores a thread)
+    const int64_t parts = (pieces + 512 * U - 1) / (512 * U);
+    const int threads = several ? 256 : (int)(((pieces + U * parts - 1) / (U * parts) + 31) / 32 * 32);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(several ? 1u : (unsigned)parts, (unsigned)std::min<int64_t>(several ? (p.M + 7) / 8 : p.M, 65535), 1);
     cfg.blockDim = dim3((unsigned)threads, 1, 1);
@@ -308,7 +317,7 @@ static int expand_rows(const Fp4ExpandParams& p, cudaStream_t stream) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     ProfScope prof(kProfPrepare, stream);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, several ? fp4_expand_kernel<T, NV, 8> : fp4_expand_kernel<T, NV, 1>, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, several ? fp4_expand_kernel<T, NV, 8, 2> : fp4_expand_kernel<T, NV, 1, U>, p);
     if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e); }
     return after_launch();
 }

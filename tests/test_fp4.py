@@ -109,3 +109,87 @@ def test_binding_refuses_what_the_library_cannot_see():
         _h, N, K = 1, 64, 64
     with pytest.raises((AttributeError, TypeError)):
         bwla._calls.fp4_linear(Other(), x.bfloat16(), x.bfloat16(), x)
+
+
+PLANS = r"""
+#include "host_plans.h"
+#include <cstdio>
+#include <vector>
+using namespace bwla;
+// The pieces of fp4_pair_kernel: every k-block of every tile belongs to one piece, the pairs that it works out for a cut tile are those that
+// have parts of it, nobody leaves two sums in one place, and counters fit the status words.
+static bool pieces(const Fp4PairPlan& r, int tiles, int kblocks) {
+    std::vector<std::vector<int>> owner(tiles, std::vector<int>(kblocks, -1));
+    const int pairs = r.pairs, rest_tiles = tiles - r.whole * pairs;
+    const int64_t rest = (int64_t)rest_tiles * kblocks;
+    if (rest_tiles < 0) return false;
+    for (int pair = 0; pair < pairs; ++pair) {
+        const int s0 = r.cut ? (int)(rest * pair / pairs) : std::min(pair, rest_tiles) * kblocks;
+        const int s1 = r.cut ? (int)(rest * (pair + 1) / pairs) : std::min(pair + 1, rest_tiles) * kblocks;
+        const int first = s0 / kblocks, count = r.whole + (s1 > s0 ? (s1 + kblocks - 1) / kblocks - first : 0);
+        int left[2] = {0, 0};
+        for (int i = 0; i < count; ++i) {
+            int tile, kb0 = 0, kb1 = kblocks, rt = 0;
+            if (i < r.whole) tile = pair + i * pairs;
+            else { rt = first + i - r.whole; tile = r.whole * pairs + rt; kb0 = std::max(s0 - rt * kblocks, 0); kb1 = std::min(s1 - rt * kblocks, kblocks); }
+            if (tile >= tiles || kb0 >= kb1) return false;
+            for (int kb = kb0; kb < kb1; ++kb) { if (owner[tile][kb] >= 0) return false; owner[tile][kb] = pair; }
+            if (kb1 - kb0 < kblocks) {
+                if (!r.cut) return false;
+                const int64_t begin = (int64_t)rt * kblocks;
+                const int from = (int)(((begin + 1) * pairs - 1) / rest), to = (int)(((begin + kblocks) * pairs - 1) / rest);
+                if (++left[kb0 == 0] > 1 || pair < from || pair > to || (kb0 == 0) != (pair == from) || from * 2 + 1 >= 256 - 4 * 4 || to - from + 1 > 255) return false;
+            }
+        }
+    }
+    for (int t = r.whole * pairs; t < tiles; ++t)
+        if (r.cut) {
+            const int64_t begin = (int64_t)(t - r.whole * pairs) * kblocks;
+            if (owner[t][0] != (int)(((begin + 1) * pairs - 1) / rest) || owner[t][kblocks - 1] != (int)(((begin + kblocks) * pairs - 1) / rest)) return false;
+        }
+    for (auto& t : owner) for (int o : t) if (o < 0) return false;
+    return true;
+}
+int main() {
+    int cut = 0, pairs = 0;
+    for (int64_t M : {1, 129, 256, 257, 333, 512, 1000, 1024, 2048, 4096, 9000})
+        for (int64_t N : {1, 77, 256, 1000, 2600, 4095, 5120, 8192, 25600})
+            for (int64_t K : {32, 256, 288, 1024, 5120, 11008, 25600})
+                for (int device : {74, 70, 3})
+                    for (int may : {1, 0}) {
+                        const Fp4PairPlan r = fp4_pair_plan(M, K, N, device, may);
+                        const int tiles = (int)(((M + 255) / 256) * ((N + 255) / 256)), kblocks = (int)((K + 255) / 256);
+                        if (r.pairs < 1 || r.pairs > device || (r.cut && !may) || !pieces(r, tiles, kblocks)) { std::printf("%d %d %d: %d\n", (int)M, (int)N, (int)K, device); return 0; }
+                        cut += r.cut; pairs += fp4_in_pairs(M, K, N);
+                        if (fp4_part_bytes(r) > (size_t)74 * 2 * kFp4PartBytes) return 0;
+                        for (int tok : {16, 32, 64, 128}) {
+                            const int parts = fp4_split_parts(M, K, N, tok);
+                            if (parts < 1 || parts > 8 || parts > kblocks) { std::printf("parts %d\n", parts); return 0; }
+                        }
+                    }
+    // A call for microscaled codes of rotated rows that keeps no room for fp32 outputs finds a kernel whatever x's alignment, and that kernel's places fit
+    for (int n1 = 1; n1 <= 192; ++n1)
+        for (int n2 = 8; n2 <= 256; n2 += 8) {
+            RotGeom g;
+            if (n1 * n2 % 32 || n1 * n2 > 25600 || !rot_geometry(n1, n2, &g)) continue;
+            int groups = 1;
+            const bool mma = rot_fp4_groups(g, &groups);
+            RotRowsGeom rows;
+            const bool many = rot_rows_geometry(n1, n2, 1, &rows);
+            if (many && (!rot_rows_fp4(rows) || rows.total > kRotMaxSmem || rows.exps < 2 * rows.tps * (rows.K / 16) || rows.staged)) { std::printf("rows %d x %d\n", n1, n2); return 0; }
+            if (!rot_fp4_unfused(g) && (!mma || !(many || rot_mma_always(g)))) { std::printf("unfused %d x %d\n", n1, n2); return 0; }
+            if (g.group_off % 16 || g.group_bytes % 16 || rot_fp4_group_bytes(g) % 16 || rot_fp4_group_bytes(g) < g.n1 * rot_fp4_row(g) * 4 + 2 * (g.K >> 4)) return 0;
+        }
+    std::printf("ok %d %d\n", cut > 20, pairs > 20);
+}
+"""
+
+
+def test_plans_cover_their_work(tmp_path):
+    import os
+    import subprocess
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2605_00422_b200", "csrc")
+    (tmp_path / "plans.cpp").write_text(PLANS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", csrc, "-o", str(tmp_path / "plans"), str(tmp_path / "plans.cpp")], check=True)
+    r = subprocess.run([str(tmp_path / "plans")], capture_output=True, text=True, timeout=120)
+    assert r.stdout == "ok 1 1\n", (r.returncode, r.stdout)
