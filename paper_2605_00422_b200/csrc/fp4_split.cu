@@ -36,13 +36,13 @@ int fp4_operand_maps(CUtensorMap* codes, CUtensorMap* scales, const uint8_t* c, 
 namespace fp4_split {
 constexpr int kRows = 128, kBlockK = 256, kThreads = 256;
 constexpr int kPush = 4;                                         // up to so many tokens sums are pushed
-template <bool NV, int TOK>
+template <bool NV, int TOK, bool DEEP>
 struct Sizes {
     static constexpr int atoms = NV ? 4 : 2;                     // scale tiles of 4 blocks in a k-block
     static constexpr int w_bytes = kRows * 128, a_bytes = TOK * 128, s_bytes = atoms * 512;
     static constexpr int stage = w_bytes + a_bytes + 2 * s_bytes;
     static constexpr int sums = TOK == 16 ? (kPush + kFp4MaxSplit) * kRows * 4 : 0;      // [token / S][part][row]
-    static constexpr int room = 112 * 1024;                      // of two CTAs an SM
+    static constexpr int room = (DEEP ? 224 : 112) * 1024;       // of one CTA an SM, or two
     static constexpr int stages = (room - 1024 - 512 - sums) / stage;
     static constexpr int sums_off = stages * stage;
     static constexpr int bars_off = sums_off + sums;
@@ -64,10 +64,10 @@ struct Fp4SplitParams {
     uint32_t* status;
 };
 
-template <bool NV, int TOK>
-__global__ void __launch_bounds__(fp4_split::kThreads, 2) fp4_split_kernel(const __grid_constant__ Fp4Maps maps, const __grid_constant__ Fp4SplitParams p) {
+template <bool NV, int TOK, bool DEEP>
+__global__ void __launch_bounds__(fp4_split::kThreads, DEEP ? 1 : 2) fp4_split_kernel(const __grid_constant__ Fp4Maps maps, const __grid_constant__ Fp4SplitParams p) {
     using namespace fp4_split;
-    using S = Sizes<NV, TOK>;
+    using S = Sizes<NV, TOK, DEEP>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* wbuf = smem;
@@ -147,6 +147,7 @@ __global__ void __launch_bounds__(fp4_split::kThreads, 2) fp4_split_kernel(const
                 if (!wait_or_abort(&full[s], ph, abort_flag)) { give_up(p.status, abort_flag, 0x320); ok = false; break; }
                 tc_fence_after();
                 const uint32_t sfw = tmem + S::sf_col + (i & 1) * (2 * 4 * S::atoms), sfa = sfw + 4 * S::atoms;
+                const uint32_t own = sfa + ((t0 & 127) >> 5);      // (a column has the scales of 32 of the scale tile's 128 tokens; it has to be an even one)
 #pragma unroll
                 for (int j = 0; j < S::atoms; ++j) {
                     tc_copy_scales<false>(sfw + 4 * j, ws_desc0 + (uint64_t)((s * S::s_bytes + j * 512) >> 4));
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(fp4_split::kThreads, 2) fp4_split_kernel(const
                 const uint64_t wd = w_desc0 + (uint64_t)((s * S::w_bytes) >> 4), ad = a_desc0 + (uint64_t)((s * S::a_bytes) >> 4);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    mma_fp4_ss<false, NV>(tmem, wd + 2 * j, ad + 2 * j, idesc_fp4(128, TOK, NV, NV ? 0 : 2 * (j & 1)), sfw + 4 * (NV ? j : j / 2), sfa + 4 * (NV ? j : j / 2),
+                    mma_fp4_ss<false, NV>(tmem, wd + 2 * j, ad + 2 * j, idesc_fp4(128, TOK, NV, NV ? 0 : 2 * (j & 1)), sfw + 4 * (NV ? j : j / 2), own + 4 * (NV ? j : j / 2),
                                           (i | j) ? 1u : 0u);
                 tc_commit(&empty[s]);
                 if (++s == S::stages) { s = 0; ph ^= 1; }
@@ -255,26 +256,25 @@ __global__ void __launch_bounds__(fp4_split::kThreads, 2) fp4_split_kernel(const
     if (!push && parts > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
 }
 
-template <bool NV, int TOK>
-static int launch_split(const Fp4GemmArgs& a, cudaStream_t stream) {
+template <bool NV, int TOK, bool DEEP>
+static int launch_split(const Fp4GemmArgs& a, int parts, cudaStream_t stream) {
     using namespace fp4_split;
-    using S = Sizes<NV, TOK>;
+    using S = Sizes<NV, TOK, DEEP>;
     Fp4Maps maps;
     int st = fp4_operand_maps(&maps.w, &maps.w_scales, a.w_codes, a.w_scales, a.N, a.K, a.format, kRows, 1);
     if (st == BWLA_OK) st = fp4_operand_maps(&maps.a, &maps.a_scales, a.a_codes, a.a_scales, a.M, a.K, a.format, TOK, 1);
     if (st != BWLA_OK) return st;
     const int64_t row_tiles = (a.N + kRows - 1) / kRows, tok_tiles = (a.M + TOK - 1) / TOK;
-    if (tok_tiles > 65535) return BWLA_ERR_INVALID_ARG;
+    if (tok_tiles > 65535 || (TOK < 64 && tok_tiles > 1)) return BWLA_ERR_INVALID_ARG;      // (the plan makes neither)
     Fp4SplitParams p{};
     p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + kBlockK - 1) / kBlockK);
     p.once = tok_tiles == 1; p.a_rows = a.a_rows; p.w_rows = a.w_rows; p.out = a.out; p.ldo = a.ldo; p.status = a.status;
     p.vec = (reinterpret_cast<uintptr_t>(a.out) & 7) == 0 && a.ldo % 4 == 0;
-    const int parts = fp4_split_parts(a.M, a.K, a.N, TOK);
     static thread_local int configured = -1;
     int dev = 0;
     BWLA_CUDA_TRY(cudaGetDevice(&dev));
     if (configured != dev) {
-        BWLA_CUDA_TRY(cudaFuncSetAttribute(fp4_split_kernel<NV, TOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::total));
+        BWLA_CUDA_TRY(cudaFuncSetAttribute(fp4_split_kernel<NV, TOK, DEEP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::total));
         configured = dev;
     }
     cudaLaunchConfig_t cfg{};
@@ -290,15 +290,20 @@ static int launch_split(const Fp4GemmArgs& a, cudaStream_t stream) {
     cfg.attrs = attrs;
     cfg.numAttrs = parts > 1 ? 2 : 1;
     ProfScope prof(kProfContraction, stream);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fp4_split_kernel<NV, TOK>, maps, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fp4_split_kernel<NV, TOK, DEEP>, maps, p);
     if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e); }
     return after_launch();
 }
 
 template <bool NV>
 static int launch_format(const Fp4GemmArgs& a, cudaStream_t stream) {
-    return a.M <= 16 ? launch_split<NV, 16>(a, stream) : a.M <= 32 ? launch_split<NV, 32>(a, stream) : a.M <= 64 ? launch_split<NV, 64>(a, stream)
-                                                                                                             : launch_split<NV, 128>(a, stream);
+    const Fp4SplitPlan r = fp4_split_plan(a.M, a.K, a.N, NV);
+    switch (r.tok) {
+        case 16: return launch_split<NV, 16, false>(a, r.parts, stream);
+        case 32: return launch_split<NV, 32, false>(a, r.parts, stream);
+        case 64: return r.deep ? launch_split<NV, 64, true>(a, r.parts, stream) : launch_split<NV, 64, false>(a, r.parts, stream);
+        default: return r.deep ? launch_split<NV, 128, true>(a, r.parts, stream) : launch_split<NV, 128, false>(a, r.parts, stream);
+    }
 }
 size_t fp4_gemm_part_bytes(int64_t M, int64_t K, int64_t N) { return fp4_in_pairs(M, K, N) ? fp4_part_bytes(fp4_pair_plan(M, K, N, kFp4Pairs, true)) : 0; }
 int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream) {

@@ -254,6 +254,32 @@ inline int fp4_split_parts(int64_t M, int64_t K, int64_t N, int tok) {
     if (cut * tiles > kFp4Sms && 4 * cut > kblocks) cut = std::max<int64_t>(kFp4Sms / tiles, kblocks / 4);
     return (int)std::max<int64_t>(1, cut);
 }
+// Tokens of a tile, parts of K, and whether a CTA has the shared memory of two (six stages of 128 tokens instead of three: one CTA with three keeps
+// 45 bytes a cycle on their way, where the L2 gives 60).  Up to 32 tokens one tile and fp4_split_parts.  More: the shortest estimate, in cycles.
+// What decides is the sums of parts, which come from the other CTAs at some 9 bytes a cycle: 128 tokens of 4096 x 4096 in one tile and four parts spent 5800 of
+// 14000 cycles on them, two tiles of 64 read the weights twice (from the L2) and have none.  (Tiles of 32 are never beside one another: the second's
+// scales would start in an odd column of tensor memory, which tcgen05.mma does not take.)
+struct Fp4SplitPlan { int tok, parts; bool deep; int64_t cycles; };
+inline Fp4SplitPlan fp4_split_plan(int64_t M, int64_t K, int64_t N, bool nv) {
+    const int64_t row_tiles = (N + 127) / 128, kblocks = (K + 255) / 256;
+    Fp4SplitPlan best{};
+    for (int tok = M <= 16 ? 16 : M <= 32 ? 32 : 64; tok <= 128; tok *= 2) {
+        const int64_t tiles = row_tiles * ((M + tok - 1) / tok), live = std::min<int64_t>(tok, M);
+        const int64_t bytes = 16384 + tok * 128 + (nv ? 4096 : 2048);
+        for (int64_t parts = 1; parts <= std::min<int64_t>(kFp4MaxSplit, kblocks); ++parts) {
+            const int64_t ctas = tiles * parts, turns = (ctas + kFp4Sms - 1) / kFp4Sms;
+            if (parts > 1 && ctas > 13 * kFp4Sms / 8) break;
+            const bool deep = tok >= 64 && turns == 1;
+            const int64_t load = turns * ((kblocks + parts - 1) / parts) * bytes / (deep || turns > 1 ? 60 : 43);
+            const int64_t memory = (N + M) * K * (nv ? 9 : 8) / 16 / 3400;
+            const int64_t last = live * 18 + (parts > 1 ? 2700 + live * 512 * (parts - 1) / parts / 9 : 500);
+            const int64_t cycles = 2500 + std::max(load, memory) + last;
+            if (!best.tok || cycles < best.cycles) best = Fp4SplitPlan{tok, (int)parts, deep, cycles};
+        }
+        if (M <= 32) { best.parts = fp4_split_parts(M, K, N, tok); return best; }
+    }
+    return best;
+}
 // Pairs, whole tiles of each, and whether the rest is cut by k: the last full round with what does not fill a round, or tiles in two where there
 // are no more than half as many as pairs.  A cut costs some 10 us (the sums of parts go through the L2), so it has to save more: time in ns.
 struct Fp4PairPlan { int pairs, whole; bool cut; int64_t ns; };
@@ -276,9 +302,7 @@ inline size_t fp4_part_bytes(const Fp4PairPlan& r) { return r.cut ? (size_t)r.pa
 inline bool fp4_in_pairs(int64_t M, int64_t K, int64_t N) {
     if (M <= 128) return false;
     if ((M + 127) / 128 > 65535) return true;            // (what a grid's second dimension holds)
-    const int64_t tiles = (N + 127) / 128 * ((M + 127) / 128), kblocks = (K + 255) / 256, parts = fp4_split_parts(M, K, N, 128);
-    const int64_t split = 6500 + (tiles * parts + kFp4Sms - 1) / kFp4Sms * ((kblocks + parts - 1) / parts) * 300;
-    return fp4_pair_plan(M, K, N, kFp4Pairs, true).ns < split;
+    return fp4_pair_plan(M, K, N, kFp4Pairs, true).ns < fp4_split_plan(M, K, N, false).cycles * 10 / 19;
 }
 
 // ---- rotation of many tokens on tcgen05 (rot_umma.cu) ----

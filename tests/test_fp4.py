@@ -162,6 +162,11 @@ int main() {
                         if (r.pairs < 1 || r.pairs > device || (r.cut && !may) || !pieces(r, tiles, kblocks)) { std::printf("%d %d %d: %d\n", (int)M, (int)N, (int)K, device); return 0; }
                         cut += r.cut; pairs += fp4_in_pairs(M, K, N);
                         if (fp4_part_bytes(r) > (size_t)74 * 2 * kFp4PartBytes) return 0;
+                        for (int nv : {0, 1}) {      // (tiles beside one another start in even columns of their scales: at multiples of 64 tokens)
+                            const Fp4SplitPlan q = fp4_split_plan(M, K, N, nv);
+                            if ((q.tok != 16 && q.tok != 32 && q.tok != 64 && q.tok != 128) || (q.tok < 64 && M > q.tok) || q.parts < 1 || q.parts > std::min(8, kblocks) ||
+                                (q.deep && q.tok < 64)) { std::printf("split %d\n", q.tok); return 0; }
+                        }
                         for (int tok : {16, 32, 64, 128}) {
                             const int parts = fp4_split_parts(M, K, N, tok);
                             if (parts < 1 || parts > 8 || parts > kblocks) { std::printf("parts %d\n", parts); return 0; }
