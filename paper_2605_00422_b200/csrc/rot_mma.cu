@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
 #pragma unroll
                         for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(acc[j][i]) & 0x7FFFFFFFu);
                     publish(sh.amax[par], __reduce_max_sync(0xFFFFFFFFu, top));
-                } else {
+                } else if (g.dc > 1) {
                     // exponents of the largest of 16 values, to all CTAs of the token: a block of 32 may have its halves in two
                     barrier();
                     for (int i = tid; i < g.n1 * y_tiles; i += T) {
@@ -583,8 +583,7 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
                             m = max(max(m, max(u.x & 0x7FFFFFFFu, u.y & 0x7FFFFFFFu)), max(u.z & 0x7FFFFFFFu, u.w & 0x7FFFFFFFu));
                         }
                         const uint32_t to = smem_u32(exps + par * (g.K >> 4) + ((c * g.n2 + rank * g.dtc * 16) >> 4) + dl);
-                        if (g.dc == 1) st_shared_u8(to, m >> 23);
-                        else for (int r = 0; r < g.dc; ++r) st_shared_cluster_u8(map_shared_rank(to, (uint32_t)r), m >> 23);
+                        for (int r = 0; r < g.dc; ++r) st_shared_cluster_u8(map_shared_rank(to, (uint32_t)r), m >> 23);
                     }
                 }
             }
@@ -785,8 +784,27 @@ __global__ void __launch_bounds__(32 * kRotMaxWarps, 1) rot_mma_kernel(const __g
                     b = fp4_block_nv<true>(bad ? 0.f : __uint_as_float(m), to_row);
                     put_scale(k16, b.byte);
                 } else {
-                    const uint16_t two = *reinterpret_cast<const volatile uint16_t*>(exps + par * (g.K >> 4) + (k16 & ~1));
-                    b = fp4_block_mx(__uint_as_float(max((uint32_t)two & 0xFFu, (uint32_t)two >> 8) << 23));
+                    uint32_t ex;
+                    if (g.dc > 1) {
+                        const uint16_t two = *reinterpret_cast<const volatile uint16_t*>(exps + par * (g.K >> 4) + (k16 & ~1));
+                        ex = max((uint32_t)two & 0xFFu, (uint32_t)two >> 8);
+                    } else {
+                        // the other half of the block, which may be the end of the row before or the beginning of the next
+                        int oc = c, od = dl + 1 - 2 * (k16 & 1);
+                        if (od < 0) { --oc; od = y_tiles - 1; }
+                        if (od == y_tiles) { ++oc; od = 0; }
+                        const uint4* half = reinterpret_cast<const uint4*>(ybuf + oc * y_row + 16 * od);
+                        uint32_t m = 0u;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint4 u = half[q];
+                            m = max(max(m, max(u.x & 0x7FFFFFFFu, u.y & 0x7FFFFFFFu)), max(u.z & 0x7FFFFFFFu, u.w & 0x7FFFFFFFu));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) m = max(m, __float_as_uint(f[e >> 3][e & 7]) & 0x7FFFFFFFu);
+                        ex = m >> 23;
+                    }
+                    b = fp4_block_mx(__uint_as_float(ex << 23));
                     if ((k16 & 1) == 0) put_scale(k16 >> 1, b.byte);
                 }
                 uint32_t word[2];

@@ -128,7 +128,6 @@ __device__ __forceinline__ void st_shared_cluster_u32(uint32_t addr, uint32_t v)
 __device__ __forceinline__ void st_shared_cluster_u8(uint32_t addr, uint32_t v) {
     asm volatile("st.shared::cluster.u8 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
-__device__ __forceinline__ void st_shared_u8(uint32_t addr, uint32_t v) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 // Arrive on an mbarrier of another CTA of the cluster (address from map_shared_rank); this thread's earlier writes,
 // remote ones included, are visible to whoever then sees the phase complete with the cluster-scope wait below.
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
