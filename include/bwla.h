@@ -317,7 +317,8 @@ int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx,
 /*
  * A prepared 4-bit layer: the factors in the form the kernels read (in `prepared`, 256-byte aligned, of
  * bwla_fp4_layer_prepared_bytes) and the caller's quantised weights of the rotated coordinates, N rows.  As for bwla_layer, the
- * handle owns no device memory and the caller keeps all of it alive and unchanged until bwla_fp4_layer_destroy.
+ * handle owns no device memory and the caller keeps all of it alive and unchanged until bwla_fp4_layer_destroy.  The calls
+ * below run on the device that was current at its creation and answer BWLA_ERR_INVALID_ARG where another one is.
  *   bwla_fp4_layer_rotate_quant  what bwla_rotate_quant_fp4 computes
  *   bwla_fp4_layer_linear        out[t][n] = the product of the quantised Y_t with the weights, one call; workspace of
  *                                bwla_fp4_layer_workspace_bytes, its first 256 bytes as above

@@ -474,6 +474,16 @@ def _fp4_need(t: torch.Tensor, dtype, name: str, ndim: int):
         raise TypeError(f"{name}: expected a tensor of the current CUDA device")
 
 
+def _fp4_factors(P1: torch.Tensor, P2: torch.Tensor):
+    for P, name in ((P1, "P1"), (P2, "P2")):
+        if P.dim() != 2 or P.shape[0] != P.shape[1]:
+            raise TypeError(f"{name}: expected a square matrix")
+    for P, name in ((P1, "P1"), (P2, "P2")):
+        _fp4_need(P, torch.float32, name, 2)
+        if not P.is_contiguous():
+            raise TypeError(f"{name} must be contiguous")
+
+
 def _fp4_stride(x: torch.Tensor) -> int:
     """Elements from a row to the next; of a single row, whose stride may be anything, at least its length."""
     return x.stride(0) if x.shape[0] > 1 else max(x.stride(0) if x.shape[0] else 0, x.shape[1])
@@ -505,11 +515,8 @@ def bwla_rotate_quant_fp4_workspace_bytes(M: int, K: int, n1: int, n2: int) -> i
 
 def bwla_rotate_quant_fp4(x: torch.Tensor, P1: torch.Tensor, P2: torch.Tensor, format: int, workspace: Optional[torch.Tensor] = None):
     """x: bf16 [M][K] -> (codes, scale tiles, row scales or None) of the rows rotated by P1 (x) P2."""
+    _fp4_factors(P1, P2)
     _fp4_need(x, torch.bfloat16, "x", 2)
-    _fp4_need(P1, torch.float32, "P1", 2)
-    _fp4_need(P2, torch.float32, "P2", 2)
-    if not (P1.is_contiguous() and P2.is_contiguous()):
-        raise TypeError("P1 and P2 must be contiguous")
     M, K = x.shape
     if workspace is None:
         workspace = _fp4_scratch(bwla_rotate_quant_fp4_workspace_bytes(M, K, P1.shape[0], P2.shape[0]), x.device)
@@ -525,14 +532,13 @@ class Fp4Layer:
     """A prepared 4-bit layer (bwla_fp4_layer_create): keeps the handle, the tensors it points into and the prepared buffer."""
 
     def __init__(self, P1, P2, format, w_codes, w_scales, w_rows=None):
-        _fp4_need(P1, torch.float32, "P1", 2)
-        _fp4_need(P2, torch.float32, "P2", 2)
+        _fp4_factors(P1, P2)
         _fp4_need(w_codes, torch.uint8, "w_codes", 2)
         _fp4_need(w_scales, torch.uint8, "w_scales", 1)
         if w_rows is not None:
             _fp4_need(w_rows, torch.float32, "w_rows", 1)
-        if not (w_codes.is_contiguous() and P1.is_contiguous() and P2.is_contiguous()):
-            raise TypeError("w_codes, P1 and P2 must be contiguous")
+        if not w_codes.is_contiguous():
+            raise TypeError("w_codes must be contiguous")
         self.N, self.K, self.format = w_codes.shape[0], 2 * w_codes.shape[1], format
         self.n1, self.n2 = P1.shape[0], P2.shape[0]
         if w_scales.numel() < bwla_fp4_scale_bytes(self.N, self.K, format) or (w_rows is not None and w_rows.numel() != self.N):

@@ -21,13 +21,22 @@ static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 // A prepared layer: the factors in the forms the rotation kernels read, and the caller's quantised weights.
 struct bwla_fp4_layer {
     int64_t K, N;
-    int n1, n2, format;
+    int n1, n2, format, device;
     const float *P1, *P2;
     const uint8_t *w_codes, *w_scales; const float* w_rows;
     PreparedFactors factors;
 };
 
 namespace bwla {
+
+// The device of a layer's weights and factors has to be the current one.
+static int check_layer_device(const bwla_fp4_layer* L) {
+    const int st = check_device();
+    if (st != BWLA_OK) return st;
+    int device = -1;
+    BWLA_CUDA_TRY(cudaGetDevice(&device));
+    return device == L->device ? BWLA_OK : BWLA_ERR_INVALID_ARG;
+}
 
 // What the rotation needs beside its outputs: status words, and room for its fp32 outputs (with 8-bit codes and scales that nobody reads) where
 // a call may go to a kernel that has no microscaled codes.
@@ -158,7 +167,9 @@ int bwla_fp4_layer_create(bwla_fp4_layer** layer, int64_t K, int64_t N, const fl
     if (!rot_geometry(n1, n2, &geom)) return BWLA_ERR_UNSUPPORTED;
     bwla_fp4_layer* L = (bwla_fp4_layer*)malloc(sizeof(bwla_fp4_layer));
     if (!L) return BWLA_ERR_INVALID_ARG;
-    *L = bwla_fp4_layer{K, N, n1, n2, format, P1, P2, w_codes, w_scales, w_rows, PreparedFactors{}};
+    int device = 0;
+    cudaGetDevice(&device);                     // (check_device has had an answer)
+    *L = bwla_fp4_layer{K, N, n1, n2, format, device, P1, P2, w_codes, w_scales, w_rows, PreparedFactors{}};
     st = prepare_factors(n1, n2, P1, P2, (uint8_t*)prepared, &L->factors, (cudaStream_t)stream);
     if (st != BWLA_OK) { free(L); return st; }
     *layer = L;
@@ -186,7 +197,7 @@ int bwla_fp4_layer_rotate_quant(const bwla_fp4_layer* L, const void* x_bf16, int
     if (M == 0) return BWLA_OK;
     if (!x_bf16 || !codes || !scales || (L->format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales)) return BWLA_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < rot_layout_of(L->factors.geom, M).total) return BWLA_ERR_WORKSPACE;
-    const int st = check_device();
+    const int st = check_layer_device(L);
     if (st != BWLA_OK) return st;
     return rotate_quant(L->factors, L->P1, L->P2, x_bf16, M, ldx, L->format, codes, scales, row_scales, workspace, false, (cudaStream_t)stream);
 }
@@ -198,7 +209,7 @@ int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M
     if (M == 0) return BWLA_OK;
     if (!x_bf16 || !out_bf16 || ((uintptr_t)out_bf16 & 1)) return BWLA_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < bwla_fp4_layer_workspace_bytes(L, M)) return BWLA_ERR_WORKSPACE;
-    int st = check_device();
+    int st = check_layer_device(L);
     if (st != BWLA_OK) return st;
     char* base = (char*)workspace;
     uint8_t* codes = (uint8_t*)(base + layer_codes_at(L, M));

@@ -264,6 +264,7 @@ inline Fp4SplitPlan fp4_split_plan(int64_t M, int64_t K, int64_t N, bool nv) {
     const int64_t row_tiles = (N + 127) / 128, kblocks = (K + 255) / 256;
     Fp4SplitPlan best{};
     for (int tok = M <= 16 ? 16 : M <= 32 ? 32 : 64; tok <= 128; tok *= 2) {
+        if (tok == 64 && (M + 63) / 64 > 65535) continue;        // (what a grid's second dimension holds)
         const int64_t tiles = row_tiles * ((M + tok - 1) / tok), live = std::min<int64_t>(tok, M);
         const int64_t bytes = 16384 + tok * 128 + (nv ? 4096 : 2048);
         for (int64_t parts = 1; parts <= std::min<int64_t>(kFp4MaxSplit, kblocks); ++parts) {
@@ -296,12 +297,12 @@ inline Fp4PairPlan fp4_pair_plan(int64_t M, int64_t K, int64_t N, int device_pai
     return r;
 }
 inline size_t fp4_part_bytes(const Fp4PairPlan& r) { return r.cut ? (size_t)r.pairs * 2 * kFp4PartBytes : 0; }
-// Which of the two takes a product.  us, fp4_split.cu | fp4_pair.cu (MX; * cut): 257 x 4096 x 4096 (tokens x K x N) 11.4 | 12; 333 x 11008 x 4096 19.3 | 24.5;
-// 512 x 4096 x 4096 11.5 | 11.8; 200 x 25600 x 5120 25.6 | 34 *; 512 x 5120 x 25600 45 | 35; 1024 x 25600 x 5120 104 | 54 *; 2048 x 5120 x 8192 56 | 37; 4096 x 5120 x
-// 25600 318 | 188.
+// Which of the two takes a product.  us, fp4_split.cu | fp4_pair.cu (MX; * cut): 257 x 4096 x 4096 (tokens x K x N) 6.8 | 12; 333 x 11008 x 4096 14.2 | 24.5;
+// 512 x 4096 x 4096 7.8 | 11.8; 200 x 25600 x 5120 23.7 | 34 *; 512 x 5120 x 25600 45 | 35; 1024 x 25600 x 5120 104 | 55 *; 2048 x 5120 x 8192 56 | 34; 4096 x 5120 x
+// 25600 318 | 194 (without a flush of the L2 between calls).
 inline bool fp4_in_pairs(int64_t M, int64_t K, int64_t N) {
     if (M <= 128) return false;
-    if ((M + 127) / 128 > 65535) return true;            // (what a grid's second dimension holds)
+    if ((M + 127) / 128 > 65535) return true;            // (the same of tiles of 128)
     return fp4_pair_plan(M, K, N, kFp4Pairs, true).ns < fp4_split_plan(M, K, N, false).cycles * 10 / 19;
 }
 

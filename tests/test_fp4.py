@@ -111,6 +111,19 @@ def test_binding_refuses_what_the_library_cannot_see():
         bwla._calls.fp4_linear(Other(), x.bfloat16(), x.bfloat16(), x)
 
 
+def test_factors_that_are_not_square_are_refused():
+    """The library reads n1 x n1 and n2 x n2 values."""
+    import torch
+
+    from paper_2605_00422_b200 import bwla
+    x, eye = torch.zeros(2, 64, dtype=torch.bfloat16), torch.eye(8)
+    w = torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8)
+    for P1, P2, name in ((eye[:, :4].contiguous(), eye, "P1"), (eye, eye[:, :4].contiguous(), "P2"), (eye[0], eye, "P1")):
+        for call in (lambda: bwla.bwla_rotate_quant_fp4(x, P1, P2, 0, workspace=w[0].view(-1)), lambda: bwla.bwla_fp4_layer_create(P1, P2, 0, *w)):
+            with pytest.raises(TypeError, match=f"{name}: expected a square matrix"):
+                call()
+
+
 PLANS = r"""
 #include "host_plans.h"
 #include <cstdio>
