@@ -301,7 +301,7 @@ inline size_t fp4_part_bytes(const Fp4PairPlan& r) { return r.cut ? (size_t)r.pa
 // 512 x 4096 x 4096 7.8 | 11.8; 200 x 25600 x 5120 23.7 | 34 *; 512 x 5120 x 25600 45 | 35; 1024 x 25600 x 5120 104 | 55 *; 2048 x 5120 x 8192 56 | 34; 4096 x 5120 x
 // 25600 318 | 194 (without a flush of the L2 between calls).
 inline bool fp4_in_pairs(int64_t M, int64_t K, int64_t N) {
-    if (M <= 128) return false;
+    if (M <= 128 || N <= 0) return false;                // (without weight rows there is no tile to plan for)
     if ((M + 127) / 128 > 65535) return true;            // (the same of tiles of 128)
     return fp4_pair_plan(M, K, N, kFp4Pairs, true).ns < fp4_split_plan(M, K, N, false).cycles * 10 / 19;
 }

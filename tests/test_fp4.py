@@ -211,3 +211,15 @@ def test_plans_cover_their_work(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-I", csrc, "-o", str(tmp_path / "plans"), str(tmp_path / "plans.cpp")], check=True)
     r = subprocess.run([str(tmp_path / "plans")], capture_output=True, text=True, timeout=120)
     assert r.stdout == "ok 1 1\n", (r.returncode, r.stdout)
+
+
+def test_workspace_of_products_without_outputs():
+    """N == 0 is a no-op for any number of tokens, its workspace the status words alone; in a process of its own, which a division by zero would end."""
+    import os
+    import subprocess
+    import sys
+    code = ("from paper_2605_00422_b200 import bwla\n"
+            "print(*[bwla.bwla_fp4_gemm_workspace_bytes(M, K, 0) for M in (0, 1, 128, 129, 4096, 100000) for K in (64, 5120)])\n"
+            "print(*[bwla._lib.bwla_fp4_gemm_codes(256, 256, None, M, 64, 256, 256, None, 0, 0, 256, 0, 256, 256, None) for M in (1, 129, 4096)])\n")
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and r.stdout.split("\n")[:2] == [" ".join(["256"] * 12), "0 0 0"], (r.returncode, r.stdout, r.stderr)

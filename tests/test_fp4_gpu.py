@@ -562,3 +562,14 @@ def test_rotated_weights_without_a_synchronisation(bwla, fmt, n1, n2):
         got = [bwla.bwla_fp4_gemm_codes(*a, *bwla.bwla_rotate_quant_fp4(W, P1, P2, FORMATS[fmt], workspace=ws2), FORMATS[fmt], workspace=ws) for W in Ws]
         torch.cuda.synchronize()
         assert all(torch.equal(u, v) for u, v in zip(got, want))
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M", [1, 128, 129, 1000])
+def test_products_without_outputs(bwla, fmt, M):
+    """No weight rows: an [M][0] tensor, with a workspace and without."""
+    K = 64
+    a = bwla.bwla_fp4_quantize_rows(torch.randn(M, K, device="cuda"), FORMATS[fmt])
+    w = bwla.bwla_fp4_quantize_rows(torch.empty(0, K, device="cuda"), FORMATS[fmt])
+    for ws in (None, bwla.new_fp4_workspace(M, K, 0)):
+        assert bwla.bwla_fp4_gemm_codes(*a, *w, FORMATS[fmt], workspace=ws).shape == (M, 0)
