@@ -294,7 +294,7 @@ int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const floa
  * of 2^-23 of its largest partial sum).
  *   out_bf16  device, bf16 [M][ldo], ldo >= N; columns beyond N are left as they are.  M == 0 or N == 0 is a no-op.
  *   workspace device, 256-byte aligned, of bwla_fp4_gemm_workspace_bytes; its first 256 bytes (status words) must be zero
- *     before the first call; bwla_check_status applies to it
+ *     before the first call; bwla_check_status applies to it.  What is allocated for M tokens serves every smaller number of them.
  */
 size_t bwla_fp4_gemm_workspace_bytes(int64_t M, int64_t K, int64_t N);
 int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_rows, int64_t M, int64_t K,
@@ -321,7 +321,8 @@ int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx,
  * below run on the device that was current at its creation and answer BWLA_ERR_INVALID_ARG where another one is.
  *   bwla_fp4_layer_rotate_quant  what bwla_rotate_quant_fp4 computes
  *   bwla_fp4_layer_linear        out[t][n] = the product of the quantised Y_t with the weights, one call; workspace of
- *                                bwla_fp4_layer_workspace_bytes, its first 256 bytes as above
+ *                                bwla_fp4_layer_workspace_bytes, its first 256 bytes as above; what is allocated for M tokens
+ *                                serves every smaller number of them
  */
 typedef struct bwla_fp4_layer bwla_fp4_layer;
 size_t bwla_fp4_layer_prepared_bytes(int64_t K, int n1, int n2);

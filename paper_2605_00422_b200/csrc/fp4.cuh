@@ -167,7 +167,7 @@ struct Fp4GemmArgs {
     uint32_t* status;
     float* parts; size_t part_bytes;      // room for sums of parts of tiles (fp4_pair.cu)
 };
-// Bytes of it that a product may use
+// Bytes of it that this product uses (fp4_part_bytes_up_to: any of up to so many tokens)
 size_t fp4_gemm_part_bytes(int64_t M, int64_t K, int64_t N);
 int launch_fp4_gemm(const Fp4GemmArgs& a, cudaStream_t stream);
 int launch_fp4_pair(const Fp4GemmArgs& a, cudaStream_t stream);

@@ -105,7 +105,7 @@ int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const floa
 
 size_t bwla_fp4_gemm_workspace_bytes(int64_t M, int64_t K, int64_t N) {
     if (!valid_rows(M, K, BWLA_FP4_MX) || !valid_rows(N, K, BWLA_FP4_MX)) return 0;
-    return kStatusBytes + fp4_gemm_part_bytes(M, K, N);
+    return kStatusBytes + fp4_part_bytes_up_to(M, K, N);
 }
 
 int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_rows, int64_t M, int64_t K, const uint8_t* w_codes,
@@ -117,11 +117,12 @@ int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const f
     if (!a_codes || !a_scales || !w_codes || !w_scales || !out_bf16 || ldo < N || ((uintptr_t)out_bf16 & 1) || !aligned16(a_codes) || !aligned16(a_scales) || !aligned16(w_codes) ||
         !aligned16(w_scales))
         return BWLA_ERR_INVALID_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < bwla_fp4_gemm_workspace_bytes(M, K, N)) return BWLA_ERR_WORKSPACE;
+    const size_t part_bytes = fp4_gemm_part_bytes(M, K, N);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < kStatusBytes + part_bytes) return BWLA_ERR_WORKSPACE;
     const int st = check_device();
     if (st != BWLA_OK) return st;
     return launch_fp4_gemm(Fp4GemmArgs{a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, M, K, N, format, (__nv_bfloat16*)out_bf16, ldo, (uint32_t*)workspace,
-                                       (float*)((char*)workspace + kStatusBytes), fp4_gemm_part_bytes(M, K, N)},
+                                       (float*)((char*)workspace + kStatusBytes), part_bytes},
                            (cudaStream_t)stream);
 }
 
@@ -187,7 +188,7 @@ static size_t layer_parts_at(const bwla_fp4_layer* L, int64_t M) { return layer_
 
 size_t bwla_fp4_layer_workspace_bytes(const bwla_fp4_layer* L, int64_t M) {
     if (!L || M < 0 || M > kFp4MaxRows) return 0;
-    return layer_parts_at(L, M) + fp4_gemm_part_bytes(M, L->K, L->N);
+    return layer_parts_at(L, M) + fp4_part_bytes_up_to(M, L->K, L->N);      // (every section grows with M)
 }
 
 int bwla_fp4_layer_rotate_quant(const bwla_fp4_layer* L, const void* x_bf16, int64_t M, int64_t ldx, uint8_t* codes, uint8_t* scales, float* row_scales,
@@ -208,7 +209,8 @@ int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M
     if (!L || M < 0 || M > kFp4MaxRows || ldx < L->K || ldo < L->N) return BWLA_ERR_INVALID_ARG;
     if (M == 0) return BWLA_OK;
     if (!x_bf16 || !out_bf16 || ((uintptr_t)out_bf16 & 1)) return BWLA_ERR_INVALID_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < bwla_fp4_layer_workspace_bytes(L, M)) return BWLA_ERR_WORKSPACE;
+    const size_t part_bytes = fp4_gemm_part_bytes(M, L->K, L->N);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < layer_parts_at(L, M) + part_bytes) return BWLA_ERR_WORKSPACE;
     int st = check_layer_device(L);
     if (st != BWLA_OK) return st;
     char* base = (char*)workspace;
@@ -218,7 +220,7 @@ int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M
     st = rotate_quant(L->factors, L->P1, L->P2, x_bf16, M, ldx, L->format, codes, scales, rows, workspace, true, (cudaStream_t)stream);
     if (st != BWLA_OK) return st;
     return launch_fp4_gemm(Fp4GemmArgs{codes, scales, rows, L->w_codes, L->w_scales, L->w_rows, M, L->K, L->N, L->format, (__nv_bfloat16*)out_bf16, ldo,
-                                       (uint32_t*)workspace, (float*)(base + layer_parts_at(L, M)), fp4_gemm_part_bytes(M, L->K, L->N)},
+                                       (uint32_t*)workspace, (float*)(base + layer_parts_at(L, M)), part_bytes},
                            (cudaStream_t)stream);
 }
 

@@ -305,6 +305,18 @@ inline bool fp4_in_pairs(int64_t M, int64_t K, int64_t N) {
     if ((M + 127) / 128 > 65535) return true;            // (the same of tiles of 128)
     return fp4_pair_plan(M, K, N, kFp4Pairs, true).ns < fp4_split_plan(M, K, N, false).cycles * 10 / 19;
 }
+// Room for the sums of parts of every product of up to M tokens: what is allocated for the largest batch serves the smaller ones, of which others
+// may be cut (11008 -> 4096: not 4096 tokens, but 1153).  More tiles have sums in as many pairs or more, so the first cut from above is the largest;
+// whether tiles are cut repeats itself after kFp4Pairs rows of tiles.  Which kernel takes a product is only asked up to 2048 tokens (it
+// takes a microsecond, and beyond them it is nearly always the pairs).
+inline size_t fp4_part_bytes_up_to(int64_t M, int64_t K, int64_t N) {
+    if (M <= 128 || N <= 0) return 0;
+    for (int64_t t = std::min<int64_t>((M + 255) / 256, 2 * kFp4Pairs); t >= 1; --t) {
+        const Fp4PairPlan r = fp4_pair_plan(256 * t, K, N, kFp4Pairs, true);
+        if (r.cut && (t > 8 || fp4_in_pairs(std::min(M, 256 * t), K, N))) return fp4_part_bytes(r);
+    }
+    return 0;
+}
 
 // ---- rotation of many tokens on tcgen05 (rot_umma.cu) ----
 constexpr int kRotUmmaSharedBytes = 1792;      // its barriers and small per-CTA state

@@ -223,3 +223,44 @@ def test_workspace_of_products_without_outputs():
             "print(*[bwla._lib.bwla_fp4_gemm_codes(256, 256, None, M, 64, 256, 256, None, 0, 0, 256, 0, 256, 256, None) for M in (1, 129, 4096)])\n")
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert r.returncode == 0 and r.stdout.split("\n")[:2] == [" ".join(["256"] * 12), "0 0 0"], (r.returncode, r.stdout, r.stderr)
+
+
+SIZES = r"""
+#include "host_plans.h"
+#include <cstdio>
+using namespace bwla;
+// Scratch made for M tokens is enough for every smaller number of them, and never falls as M grows.
+int main() {
+    int cut = 0, kept = 0;
+    for (int64_t N : {1, 77, 256, 1000, 4096, 5120, 8192, 11008, 25600})
+        for (int64_t K : {32, 256, 2048, 5120, 8192, 11008, 25600, 65536}) {
+            size_t most = 0, before = 0;
+            for (int64_t M = 0; M <= 45000; M += M < 2500 ? 1 : 127) {
+                const size_t need = fp4_in_pairs(M, K, N) ? fp4_part_bytes(fp4_pair_plan(M, K, N, kFp4Pairs, true)) : 0, room = fp4_part_bytes_up_to(M, K, N);
+                most = std::max(most, need);
+                if (room < most || room < before || room > (size_t)kFp4Pairs * 2 * kFp4PartBytes) { std::printf("%d %d %d: %zu of %zu\n", (int)M, (int)K, (int)N, room, most); return 0; }
+                if (M <= 2048 && room != most) { std::printf("%d %d %d: %zu for %zu\n", (int)M, (int)K, (int)N, room, most); return 0; }
+                before = room; cut += need > 0; kept += room > need;
+            }
+        }
+    std::printf("ok %d %d\n", cut > 1000, kept > 1000);
+}
+"""
+
+
+def test_scratch_of_many_tokens_serves_fewer(lib, tmp_path):
+    import os
+    import subprocess
+    big = lib.bwla_fp4_gemm_workspace_bytes(4096, 11008, 4096)
+    buf = (C.c_uint8 * 4096)()
+    p = C.c_void_p((C.addressof(buf) + 255) // 256 * 256)
+    import torch
+    for M in (1, 128, 129, 1000, 1153, 2048, 3500, 4000, 4095, 4096):
+        assert lib.bwla_fp4_gemm_workspace_bytes(M, 11008, 4096) <= big
+        if not torch.cuda.is_available():      # (refused for the missing device, not for the workspace)
+            assert lib.bwla_fp4_gemm_codes(p, p, None, M, 11008, p, p, None, 4096, 0, p, 4096, p, big, None) == -2
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2605_00422_b200", "csrc")
+    (tmp_path / "sizes.cpp").write_text(SIZES)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", csrc, "-o", str(tmp_path / "sizes"), str(tmp_path / "sizes.cpp")], check=True)
+    r = subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, timeout=300)
+    assert r.stdout == "ok 1 1\n", (r.returncode, r.stdout)

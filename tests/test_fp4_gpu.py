@@ -573,3 +573,24 @@ def test_products_without_outputs(bwla, fmt, M):
     w = bwla.bwla_fp4_quantize_rows(torch.empty(0, K, device="cuda"), FORMATS[fmt])
     for ws in (None, bwla.new_fp4_workspace(M, K, 0)):
         assert bwla.bwla_fp4_gemm_codes(*a, *w, FORMATS[fmt], workspace=ws).shape == (M, 0)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_scratch_of_many_tokens_serves_fewer(bwla, fmt):
+    """One workspace, made for the largest batch, for products and layers of all smaller ones (of some of which tiles are cut by k)."""
+    rng = np.random.default_rng(11)
+    K, N, most = 11008, 4096, 4096
+    w, sw, vw = operand(rng, N, K, fmt, integers=True)
+    ws = bwla.new_fp4_workspace(most, K, N)
+    for M in (1153, 1, 3500, 129, 2100):
+        a, sa, va = operand(rng, M, K, fmt, integers=True)
+        check_product(bwla.bwla_fp4_gemm_codes(a, sa, None, w, sw, None, FORMATS[fmt], workspace=ws), va, vw, exact=True)
+        assert bwla.bwla_check_status(ws) == 0 and not ws[:256].any()
+    n1, n2 = 64, 128
+    w = bwla.bwla_fp4_quantize_rows(torch.randn(N, n1 * n2, device="cuda"), FORMATS[fmt])
+    layer = bwla.bwla_fp4_layer_create(dev(haar(rng, n1)), dev(haar(rng, n2)), FORMATS[fmt], *w)
+    ws = bwla.new_fp4_layer_workspace(layer, most)
+    for M in (3584, 1, 3500, 4096, 33):
+        x = torch.randn(M, n1 * n2, device="cuda").bfloat16()
+        assert torch.equal(bwla.bwla_fp4_layer_linear(layer, x, workspace=ws), bwla.bwla_fp4_layer_linear(layer, x))
+        assert bwla.bwla_check_status(ws) == 0
