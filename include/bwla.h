@@ -275,7 +275,8 @@ size_t bwla_fp4_scale_bytes(int64_t rows, int64_t K, int format);      /* 0 for 
  * Rows (activations or weights) to codes and scales.
  *   x     device, [M][ldx] of `dtype` (BWLA_DTYPE_F32, BF16 or F16), ldx >= K
  *   row_scales is written for BWLA_FP4_NV and not used for BWLA_FP4_MX.  M == 0 is a no-op.
- * The outputs may be weights of the next call on `stream` without a synchronisation (no call starts before this one has ended).
+ * The outputs may be weights of the next call on `stream`, a prepared layer's among them, without a synchronisation (no call starts
+ * before this one has ended).
  */
 int bwla_fp4_quantize_rows(const void* x, int dtype, int64_t M, int64_t K, int64_t ldx, int format,
                            uint8_t* codes, uint8_t* scales, float* row_scales, void* stream);
@@ -292,6 +293,7 @@ int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const floa
  *   out[m][n] = bf16( a_rows[m] * w_rows[n] * sum_k a[m][k] * w[n][k] )
  * with fp32 sums on the block-scaled tensor cores (their accumulation truncates: a sum over K is off by at most K/64 units
  * of 2^-23 of its largest partial sum).
+ * All inputs, the weights' codes and scales among them, may be what the preceding kernel of `stream` makes, whoever's kernel it is.
  *   out_bf16  device, bf16 [M][ldo], ldo >= N; columns beyond N are left as they are.  M == 0 or N == 0 is a no-op.
  *   workspace device, 256-byte aligned, of bwla_fp4_gemm_workspace_bytes; its first 256 bytes (status words) must be zero
  *     before the first call; bwla_check_status applies to it.  What is allocated for M tokens serves every smaller number of them.
@@ -317,7 +319,8 @@ int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx,
 /*
  * A prepared 4-bit layer: the factors in the form the kernels read (in `prepared`, 256-byte aligned, of
  * bwla_fp4_layer_prepared_bytes) and the caller's quantised weights of the rotated coordinates, N rows.  As for bwla_layer, the
- * handle owns no device memory and the caller keeps all of it alive and unchanged until bwla_fp4_layer_destroy.  The calls
+ * handle owns no device memory and the caller keeps all of it alive and unchanged until bwla_fp4_layer_destroy (the product reads
+ * the weights before it waits for the preceding kernel; what made them may be the kernel of `stream` before the creation).  The calls
  * below run on the device that was current at its creation and answer BWLA_ERR_INVALID_ARG where another one is.
  *   bwla_fp4_layer_rotate_quant  what bwla_rotate_quant_fp4 computes
  *   bwla_fp4_layer_linear        out[t][n] = the product of the quantised Y_t with the weights, one call; workspace of

@@ -166,6 +166,7 @@ struct Fp4GemmArgs {
     __nv_bfloat16* out; int64_t ldo;
     uint32_t* status;
     float* parts; size_t part_bytes;      // room for sums of parts of tiles (fp4_pair.cu)
+    bool prepared;                        // a layer's weights, complete before its kernels: read before griddepcontrol.wait
 };
 // Bytes of it that this product uses (fp4_part_bytes_up_to: any of up to so many tokens)
 size_t fp4_gemm_part_bytes(int64_t M, int64_t K, int64_t N);

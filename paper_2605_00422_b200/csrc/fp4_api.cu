@@ -122,7 +122,7 @@ int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const f
     const int st = check_device();
     if (st != BWLA_OK) return st;
     return launch_fp4_gemm(Fp4GemmArgs{a_codes, a_scales, a_rows, w_codes, w_scales, w_rows, M, K, N, format, (__nv_bfloat16*)out_bf16, ldo, (uint32_t*)workspace,
-                                       (float*)((char*)workspace + kStatusBytes), part_bytes},
+                                       (float*)((char*)workspace + kStatusBytes), part_bytes, false},
                            (cudaStream_t)stream);
 }
 
@@ -220,7 +220,7 @@ int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M
     st = rotate_quant(L->factors, L->P1, L->P2, x_bf16, M, ldx, L->format, codes, scales, rows, workspace, true, (cudaStream_t)stream);
     if (st != BWLA_OK) return st;
     return launch_fp4_gemm(Fp4GemmArgs{codes, scales, rows, L->w_codes, L->w_scales, L->w_rows, M, L->K, L->N, L->format, (__nv_bfloat16*)out_bf16, ldo,
-                                       (uint32_t*)workspace, (float*)(base + layer_parts_at(L, M)), part_bytes},
+                                       (uint32_t*)workspace, (float*)(base + layer_parts_at(L, M)), part_bytes, true},
                            (cudaStream_t)stream);
 }
 

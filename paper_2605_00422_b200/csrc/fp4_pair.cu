@@ -4,7 +4,7 @@
 // Bound by the tensor cores and by what feeds them: a k-block of 256 is 512 cycles of MMAs and 32 KB of codes and 3 (MX) or 6 KB (NV) of
 // scales a CTA, 70 bytes a cycle and SM from the L2.  A pair (cta_group::2) is one tensor core to the MMAs: each CTA holds 128 of the tokens
 // and 128 of the weight rows in shared memory, all 256 weight rows' scales, and the accumulators of its tokens.
-//   warp 0       TMA into a ring of stages, all tiles back to back (the weights of the first stages before griddepcontrol.wait)
+//   warp 0       TMA into a ring of stages, all tiles back to back (a layer's weights of the first stages before griddepcontrol.wait)
 //   warp 1       in the even CTA: tcgen05.cp of the scale tiles (two buffers in tensor memory), four MMAs a k-block
 //   warps 2..5   epilogue: accumulators to registers, row scales, bf16, shared memory, bulk tensor stores
 // Tensor memory holds two accumulators of 256 columns that share 96 (512 columns less the scales' 96): tile i + 1 starts when the epilogue has
@@ -49,6 +49,7 @@ struct Fp4PairParams {
     uint32_t* counters;              // arrivals at a cut tile: a byte for each pair that begins one and CTA
     const float *a_rows, *w_rows;
     __nv_bfloat16* out; int64_t ldo;
+    int prepared;                    // the weights are complete before the preceding kernel is
     int bulk;                        // rows of out in 16-byte pieces
     uint32_t* status;
 };
@@ -159,9 +160,16 @@ __global__ void __launch_bounds__(fp4_pair::kThreads, 1) fp4_pair_kernel(const _
             if (my_tiles > 0) {
                 const Piece r = piece_at(0);
                 ahead = min(r.kb1 - r.kb0, kStages);
-                for (int j = 0; j < ahead; ++j) weights(r.kb0 + j, r.n0, j);
+                for (int j = 0; j < ahead; ++j) {
+                    if (p.prepared) { weights(r.kb0 + j, r.n0, j); continue; }
+                    tma_prefetch_2d(&maps.in.w, (r.kb0 + j) * 128, r.n0 + rank * kHalf);      // (into the L2, where a kernel that still makes them writes)
+                    tma_prefetch_3d(&maps.in.w_scales, 0, (r.kb0 + j) * S::atoms, r.n0 >> 7);
+                }
                 griddep_wait();
-                for (int j = 0; j < ahead; ++j) tokens(r.kb0 + j, r.t0, j);
+                for (int j = 0; j < ahead; ++j) {
+                    if (!p.prepared) weights(r.kb0 + j, r.n0, j);
+                    tokens(r.kb0 + j, r.t0, j);
+                }
             }
             s = ahead % kStages;
             if (ahead == kStages) ph = 0;
@@ -439,7 +447,7 @@ static int launch_pair(const Fp4GemmArgs& a, cudaStream_t stream) {
     p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + kBlockK - 1) / kBlockK);
     p.tok_tiles = (int)((a.M + kTok - 1) / kTok); p.row_tiles = (int)((a.N + kRows - 1) / kRows);
     p.group = std::min(p.tok_tiles, 8);
-    p.a_rows = a.a_rows; p.w_rows = a.w_rows; p.out = a.out; p.ldo = a.ldo; p.status = a.status;
+    p.a_rows = a.a_rows; p.w_rows = a.w_rows; p.out = a.out; p.ldo = a.ldo; p.status = a.status; p.prepared = a.prepared;
     p.bulk = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0 && a.ldo % 8 == 0;
     if ((int64_t)p.tok_tiles * p.row_tiles >= ((int64_t)1 << 31)) return BWLA_ERR_INVALID_ARG;
     if (p.bulk) {

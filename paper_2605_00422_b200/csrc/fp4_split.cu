@@ -5,8 +5,9 @@
 // operand whose rows are the 128 lanes, so few tokens cost few columns; K is cut so that about two CTAs an SM stream it (the cut is what
 // fills the device: 5120 x 5120 has 40 row tiles), and the parts of a cluster meet in shared memory over the cluster, added in the order of
 // k, so a call repeats itself bit for bit.
-//   warp 0   TMA: per k-block of 256 the weights' codes (128 x 128 bytes) and scale tiles, the tokens' codes and scale tiles.  The weights of the
-//            first stages are asked for before griddepcontrol.wait: only the tokens may come from the kernel before.
+//   warp 0   TMA: per k-block of 256 the weights' codes (128 x 128 bytes) and scale tiles, the tokens' codes and scale tiles.  A layer's weights
+//            of the first stages are asked for before griddepcontrol.wait; those of a product of two operands may come from the kernel before, as
+//            the tokens may, whoever's it is: until the wait they are only asked into the L2, where its writes go.
 //   warp 1   tcgen05.cp of the scale tiles into tensor memory (two buffers), four MMAs of 64 values of k
 //   all      epilogue: token t of the tile is finished by CTA t mod S of the cluster.  The sums lie where the stages were, [token][row], and the owners
 //            read them between two cluster barriers.  Up to four tokens every CTA pushes its sums to the owners instead, who have room
@@ -58,6 +59,7 @@ struct Sizes {
 struct Fp4SplitParams {
     int M, N, kblocks;
     int once;                         // every weight is read by one tile only
+    int prepared;                     // the weights are complete before the preceding kernel is
     const float *a_rows, *w_rows;
     __nv_bfloat16* out; int64_t ldo;
     int vec;                          // rows of out in 8-byte pieces
@@ -104,7 +106,11 @@ __global__ void __launch_bounds__(fp4_split::kThreads, DEEP ? 1 : 2) fp4_split_k
         mbar_init(pushed, parts * (kThreads / 32));
         fence_barrier_init();
         fence_proxy_async();
-        for (int i = 0; i < ahead; ++i) weights(i, i);       // (they do not depend on the preceding kernel, nor on the tensor memory)
+        for (int i = 0; i < ahead; ++i) {                    // (they do not depend on the tensor memory)
+            if (p.prepared) { weights(i, i); continue; }
+            tma_prefetch_2d(&maps.w, (kb0 + i) * 128, n0);
+            tma_prefetch_3d(&maps.w_scales, 0, (kb0 + i) * S::atoms, (int)blockIdx.x);
+        }
     }
     __syncwarp();
     if (warp == 1) {
@@ -125,7 +131,10 @@ __global__ void __launch_bounds__(fp4_split::kThreads, DEEP ? 1 : 2) fp4_split_k
                 tma_load_3d(asbuf + s * S::s_bytes, &maps.a_scales, 0, (kb0 + i) * S::atoms, t0 >> 7, &full[s]);
             };
             griddep_wait();
-            for (int i = 0; i < ahead; ++i) tokens(i, i);
+            for (int i = 0; i < ahead; ++i) {
+                if (!p.prepared) weights(i, i);
+                tokens(i, i);
+            }
             int s = 0; uint32_t ph = 0;
             for (int i = ahead; i < count; ++i) {
                 if (!wait_or_abort(&empty[s], ph, abort_flag)) { give_up(p.status, abort_flag, 0x310); break; }
@@ -268,7 +277,7 @@ static int launch_split(const Fp4GemmArgs& a, int parts, cudaStream_t stream) {
     if (tok_tiles > 65535 || (TOK < 64 && tok_tiles > 1)) return BWLA_ERR_INVALID_ARG;      // (the plan makes neither)
     Fp4SplitParams p{};
     p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + kBlockK - 1) / kBlockK);
-    p.once = tok_tiles == 1; p.a_rows = a.a_rows; p.w_rows = a.w_rows; p.out = a.out; p.ldo = a.ldo; p.status = a.status;
+    p.once = tok_tiles == 1; p.prepared = a.prepared; p.a_rows = a.a_rows; p.w_rows = a.w_rows; p.out = a.out; p.ldo = a.ldo; p.status = a.status;
     p.vec = (reinterpret_cast<uintptr_t>(a.out) & 7) == 0 && a.ldo % 4 == 0;
     static thread_local int configured = -1;
     int dev = 0;

@@ -594,3 +594,43 @@ def test_scratch_of_many_tokens_serves_fewer(bwla, fmt):
         x = torch.randn(M, n1 * n2, device="cuda").bfloat16()
         assert torch.equal(bwla.bwla_fp4_layer_linear(layer, x, workspace=ws), bwla.bwla_fp4_layer_linear(layer, x))
         assert bwla.bwla_check_status(ws) == 0
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M", [1, 40, 600])
+@pytest.mark.parametrize("N,K", [(512, 1024), (1536, 2048)])
+def test_weights_made_by_a_kernel_that_lets_others_start(bwla, fmt, M, N, K):
+    """Weights' codes and scales that the kernel directly before writes, which lets the next one start at once (a product, whose outputs are
+    taken as codes: any bytes are) or is PyTorch's.  Two sets in turn, so that bytes of the round before give other outputs."""
+    rng = np.random.default_rng([M, N, K, 21])
+    a, sa, va = operand(rng, M, K, fmt)
+    makers = []
+    for _ in range(2):      # bf16 [N][K/4] are the bytes of codes [N][K/2]
+        t, st, _ = operand(rng, N, 512, fmt)
+        u, su, _ = operand(rng, K // 4, 512, fmt)
+        makers.append((t, st, None, u, su, None))
+    scales = [operand(rng, N, K, fmt)[1] for _ in range(2)]
+    bytes_ = torch.empty(N, K // 4, dtype=torch.bfloat16, device="cuda")
+    codes, sw = bytes_.view(torch.uint8), torch.empty_like(scales[0])
+    ws, ws2 = bwla.new_fp4_workspace(N, 512, K // 4), bwla.new_fp4_workspace(M, K, N)
+    want, made = [], []
+    for m, s in zip(makers, scales):
+        bwla.bwla_fp4_gemm_codes(*m, FORMATS[fmt], out=bytes_, workspace=ws)
+        torch.cuda.synchronize()
+        want.append(bwla.bwla_fp4_gemm_codes(a, sa, None, codes, s, None, FORMATS[fmt], workspace=ws2))
+        torch.cuda.synchronize()
+        made.append(codes.clone())
+    assert not torch.equal(*want)
+    torch.cuda.synchronize()
+    got = []
+    for i in range(20):
+        sw.copy_(scales[i % 2])
+        bwla.bwla_fp4_gemm_codes(*makers[i % 2], FORMATS[fmt], out=bytes_, workspace=ws)
+        got.append(bwla.bwla_fp4_gemm_codes(a, sa, None, codes, sw, None, FORMATS[fmt], workspace=ws2))
+    for i in range(20):
+        codes.copy_(made[i % 2])
+        sw.copy_(scales[i % 2])
+        got.append(bwla.bwla_fp4_gemm_codes(a, sa, None, codes, sw, None, FORMATS[fmt], workspace=ws2))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i % 2]) for i, y in enumerate(got))
+    assert bwla.bwla_check_status(ws) == 0 and bwla.bwla_check_status(ws2) == 0
