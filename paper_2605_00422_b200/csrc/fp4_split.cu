@@ -11,7 +11,7 @@
 //   warp 1   tcgen05.cp of the scale tiles into tensor memory (two buffers), four MMAs of 64 values of k
 //   all      epilogue: token t of the tile is finished by CTA t mod S of the cluster.  The sums lie where the stages were, [token][row], and the owners
 //            read them between two cluster barriers.  Up to four tokens every CTA pushes its sums to the owners instead, who have room
-//            beside their stages, and a barrier of the owner's counts them: nobody else waits (one token 4096 x 4096 4.2 -> 3.9 us, 5120 x 5120
+//            beside their stages, and a barrier of the owner's counts them: nobody else waits for sums (one token 4096 x 4096 4.2 -> 3.9 us, 5120 x 5120
 //            NV 5.7 -> 5.3; but 32 tokens of 5120 x 5120 6.2 -> 7.0: words, where reading takes 16 bytes).  Rows of 256 bytes are stored.
 #include "fp4.cuh"
 #include "tensor_map.cuh"
@@ -208,6 +208,7 @@ __global__ void __launch_bounds__(fp4_split::kThreads, DEEP ? 1 : 2) fp4_split_k
         __syncwarp();
         if (lane < owners) mbar_arrive_remote(map_shared_rank(smem_u32(pushed), (uint32_t)lane));
         __syncwarp();
+        cluster_arrive_release();                        // (this CTA stores to no other any more: see the end)
         if (rank < owners) {
             bool there = false;
             for (uint32_t i = 0; i < kWaitLimit && !there; ++i) there = __all_sync(0xFFFFFFFFu, mbar_try_wait_cluster(pushed, 0u, kParkNs));
@@ -261,8 +262,10 @@ __global__ void __launch_bounds__(fp4_split::kThreads, DEEP ? 1 : 2) fp4_split_k
         tc_fence_after();
         tmem_dealloc(tmem, S::cols);
     }
-    // nobody leaves while a neighbour still reads its sums
-    if (!push && parts > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
+    // nobody leaves while a neighbour still reads its sums, or may store to it: one whose wait for its MMAs ran out pushes late, when an owner
+    // may have stopped waiting for it
+    if (push) cluster_wait_acquire();
+    else if (parts > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
 }
 
 template <bool NV, int TOK, bool DEEP>

@@ -634,3 +634,25 @@ def test_weights_made_by_a_kernel_that_lets_others_start(bwla, fmt, M, N, K):
     torch.cuda.synchronize()
     assert all(torch.equal(y, want[i % 2]) for i, y in enumerate(got))
     assert bwla.bwla_check_status(ws) == 0 and bwla.bwla_check_status(ws2) == 0
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M", [1, 2, 3, 4])
+def test_pushed_sums_on_two_streams(bwla, fmt, M):
+    """Few tokens, K cut over clusters of every size: calls on two streams beside one another, again and again."""
+    shapes = [(256, 5120), (1000, 2048), (5120, 5120), (300, 25600)]
+    rng = np.random.default_rng([M, 31])
+    ops = [(*operand(rng, M, K, fmt, integers=True), *operand(rng, N, K, fmt, integers=True)) for N, K in shapes]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    wss = [[bwla.new_fp4_workspace(M, K, N) for N, K in shapes] for _ in streams]
+    torch.cuda.synchronize()
+    outs = []
+    for i in range(25):
+        for s, ws in zip(streams, wss):
+            with torch.cuda.stream(s):
+                outs.append([bwla.bwla_fp4_gemm_codes(a, sa, None, w, sw, None, FORMATS[fmt], workspace=x) for (a, sa, _, w, sw, _), x in zip(ops, ws)])
+    torch.cuda.synchronize()
+    for (_, _, va, _, _, vw), first, *rest in zip(ops, *outs):
+        check_product(first, va, vw, exact=True)
+        assert all(torch.equal(first, y) for y in rest)
+    assert all(bwla.bwla_check_status(x) == 0 for ws in wss for x in ws)
