@@ -267,6 +267,7 @@ int bwla_w1ax_linear_group(const bwla_layer* const* layers, int count, const voi
  *              of the same 128 rows one after the other; in a tile block j of row r is byte (r % 32) * 16 + (r / 32) * 4 + j.
  *              Blocks that fill up a row's last tile must be zero (the quantiser writes them); rows beyond the last may hold anything.
  *   row_scales fp32 [rows], or NULL for ones
+ * Pointers of the calls below that are not on a multiple of their elements' size return BWLA_ERR_INVALID_ARG.
  */
 enum { BWLA_FP4_MX = 0, BWLA_FP4_NV = 1 };
 size_t bwla_fp4_scale_bytes(int64_t rows, int64_t K, int format);      /* 0 for sizes that are not taken, or no rows */

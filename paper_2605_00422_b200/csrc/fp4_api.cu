@@ -15,6 +15,9 @@ static bool valid_rows(int64_t rows, int64_t K, int format) {
     return valid_format(format) && rows >= 0 && rows <= kFp4MaxRows && K > 0 && K % 32 == 0 && K <= kFp4MaxK;
 }
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// on whole elements of `size` bytes, as the kernels read and write them (NULL is)
+static bool on(const void* p, int size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) == 0; }
+static int dtype_size(int dtype) { return dtype == BWLA_DTYPE_F32 ? 4 : 2; }
 
 }  // namespace bwla
 
@@ -86,7 +89,8 @@ int bwla_fp4_quantize_rows(const void* x, int dtype, int64_t M, int64_t K, int64
     g_launch_count = 0;
     if (!valid_rows(M, K, format) || ldx < K || (dtype != BWLA_DTYPE_F32 && dtype != BWLA_DTYPE_BF16 && dtype != BWLA_DTYPE_F16)) return BWLA_ERR_INVALID_ARG;
     if (M == 0) return BWLA_OK;
-    if (!x || !codes || !scales || (format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales)) return BWLA_ERR_INVALID_ARG;
+    if (!x || !codes || !scales || (format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales) || !on(x, dtype_size(dtype)) || !on(row_scales, 4))
+        return BWLA_ERR_INVALID_ARG;
     const int st = check_device();
     if (st != BWLA_OK) return st;
     return launch_fp4_quantize(x, dtype, M, K, ldx, format, codes, scales, row_scales, false, (cudaStream_t)stream);
@@ -97,7 +101,7 @@ int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const floa
     g_launch_count = 0;
     if (!valid_rows(M, K, format) || ldo < K || (dtype != BWLA_DTYPE_F32 && dtype != BWLA_DTYPE_BF16)) return BWLA_ERR_INVALID_ARG;
     if (M == 0) return BWLA_OK;
-    if (!codes || !scales || !out || !aligned16(codes) || !aligned16(scales)) return BWLA_ERR_INVALID_ARG;
+    if (!codes || !scales || !out || !aligned16(codes) || !aligned16(scales) || !on(out, dtype_size(dtype)) || !on(row_scales, 4)) return BWLA_ERR_INVALID_ARG;
     const int st = check_device();
     if (st != BWLA_OK) return st;
     return launch_fp4_expand(codes, scales, row_scales, M, K, format, out, dtype, ldo, (cudaStream_t)stream);
@@ -114,8 +118,8 @@ int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const f
     g_launch_count = 0;
     if (!valid_rows(M, K, format) || !valid_rows(N, K, format)) return BWLA_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return BWLA_OK;
-    if (!a_codes || !a_scales || !w_codes || !w_scales || !out_bf16 || ldo < N || ((uintptr_t)out_bf16 & 1) || !aligned16(a_codes) || !aligned16(a_scales) || !aligned16(w_codes) ||
-        !aligned16(w_scales))
+    if (!a_codes || !a_scales || !w_codes || !w_scales || !out_bf16 || ldo < N || !on(out_bf16, 2) || !aligned16(a_codes) || !aligned16(a_scales) || !aligned16(w_codes) ||
+        !aligned16(w_scales) || !on(a_rows, 4) || !on(w_rows, 4))
         return BWLA_ERR_INVALID_ARG;
     const size_t part_bytes = fp4_gemm_part_bytes(M, K, N);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < kStatusBytes + part_bytes) return BWLA_ERR_WORKSPACE;
@@ -138,7 +142,7 @@ int bwla_rotate_quant_fp4(const void* x_bf16, int64_t M, int64_t K, int64_t ldx,
     if (!valid_rows(M, K, format) || !valid_rotation_dims(K, n1, n2) || ldx < K) return BWLA_ERR_INVALID_ARG;
     if (M == 0) return BWLA_OK;
     if (!x_bf16 || !P1 || !P2 || !codes || !scales || (format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales) || !aligned16(P1) ||
-        !aligned16(P2))
+        !aligned16(P2) || !on(x_bf16, 2) || !on(row_scales, 4))
         return BWLA_ERR_INVALID_ARG;
     PreparedFactors f{};
     const bool supported = rot_geometry(n1, n2, &f.geom);
@@ -160,7 +164,7 @@ int bwla_fp4_layer_create(bwla_fp4_layer** layer, int64_t K, int64_t N, const fl
     if (!layer) return BWLA_ERR_INVALID_ARG;
     *layer = nullptr;
     if (!valid_rotation_dims(K, n1, n2) || !valid_rows(N, K, format) || N <= 0) return BWLA_ERR_INVALID_ARG;
-    if (!P1 || !P2 || !w_codes || !w_scales || !aligned16(P1) || !aligned16(P2) || !aligned16(w_codes) || !aligned16(w_scales)) return BWLA_ERR_INVALID_ARG;
+    if (!P1 || !P2 || !w_codes || !w_scales || !aligned16(P1) || !aligned16(P2) || !aligned16(w_codes) || !aligned16(w_scales) || !on(w_rows, 4)) return BWLA_ERR_INVALID_ARG;
     if (!prepared || ((uintptr_t)prepared & 255) || prepared_bytes < bwla_fp4_layer_prepared_bytes(K, n1, n2)) return BWLA_ERR_WORKSPACE;
     int st = check_device();
     if (st != BWLA_OK) return st;
@@ -196,7 +200,8 @@ int bwla_fp4_layer_rotate_quant(const bwla_fp4_layer* L, const void* x_bf16, int
     g_launch_count = 0;
     if (!L || M < 0 || M > kFp4MaxRows || ldx < L->K) return BWLA_ERR_INVALID_ARG;
     if (M == 0) return BWLA_OK;
-    if (!x_bf16 || !codes || !scales || (L->format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales)) return BWLA_ERR_INVALID_ARG;
+    if (!x_bf16 || !codes || !scales || (L->format == BWLA_FP4_NV && !row_scales) || !aligned16(codes) || !aligned16(scales) || !on(x_bf16, 2) || !on(row_scales, 4))
+        return BWLA_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < rot_layout_of(L->factors.geom, M).total) return BWLA_ERR_WORKSPACE;
     const int st = check_layer_device(L);
     if (st != BWLA_OK) return st;
@@ -208,7 +213,7 @@ int bwla_fp4_layer_linear(const bwla_fp4_layer* L, const void* x_bf16, int64_t M
     g_launch_count = 0;
     if (!L || M < 0 || M > kFp4MaxRows || ldx < L->K || ldo < L->N) return BWLA_ERR_INVALID_ARG;
     if (M == 0) return BWLA_OK;
-    if (!x_bf16 || !out_bf16 || ((uintptr_t)out_bf16 & 1)) return BWLA_ERR_INVALID_ARG;
+    if (!x_bf16 || !out_bf16 || !on(x_bf16, 2) || !on(out_bf16, 2)) return BWLA_ERR_INVALID_ARG;
     const size_t part_bytes = fp4_gemm_part_bytes(M, L->K, L->N);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < layer_parts_at(L, M) + part_bytes) return BWLA_ERR_WORKSPACE;
     int st = check_layer_device(L);

@@ -264,3 +264,22 @@ def test_scratch_of_many_tokens_serves_fewer(lib, tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-I", csrc, "-o", str(tmp_path / "sizes"), str(tmp_path / "sizes.cpp")], check=True)
     r = subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, timeout=300)
     assert r.stdout == "ok 1 1\n", (r.returncode, r.stdout)
+
+
+def test_pointers_off_their_elements_are_refused(lib):
+    """What the kernels read or write in whole elements has to lie on them."""
+    buf = (C.c_uint8 * 4096)()
+    at = (C.addressof(buf) + 255) // 256 * 256
+    p, one, two = C.c_void_p(at), C.c_void_p(at + 1), C.c_void_p(at + 2)
+    quantize = lambda x, dtype, rows: lib.bwla_fp4_quantize_rows(x, dtype, 1, 32, 32, 1, p, p, rows, None)
+    expand = lambda out, dtype, rows: lib.bwla_fp4_expand_rows(p, p, rows, 1, 32, 1, out, dtype, 32, None)
+    gemm = lambda a, w, out: lib.bwla_fp4_gemm_codes(p, p, a, 1, 32, p, p, w, 8, 1, out, 8, p, 256, None)
+    rotate = lambda x, rows: lib.bwla_rotate_quant_fp4(x, 1, 64, 64, p, 8, p, 8, 1, p, p, rows, p, 1 << 20, None)
+    h = C.c_void_p()
+    create = lambda w: lib.bwla_fp4_layer_create(C.byref(h), 64, 8, p, 8, p, 8, 1, p, p, w, p, 1 << 20, None)
+    for st in (quantize(one, 0, p), quantize(two, 0, p), quantize(one, 1, p), quantize(one, 2, p), quantize(p, 0, two), expand(one, 0, None), expand(two, 0, None),
+               expand(one, 1, None), expand(p, 1, two), gemm(two, None, p), gemm(None, one, p), gemm(None, None, one), rotate(one, p), rotate(p, two), create(two)):
+        assert st == -1
+    import torch
+    if not torch.cuda.is_available():          # on their elements they are taken: what is refused here is the missing device
+        assert quantize(two, 1, p) == quantize(two, 2, p) == expand(two, 1, None) == gemm(None, None, two) == rotate(two, p) == create(None) == -2
