@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(256) prepare_okt_kernel(OktGeom g, const float
         for (int h = 0; h < 3; ++h)
             *reinterpret_cast<__nv_bfloat16*>(region + (size_t)(h * atoms + j) * rows * atom + in_block) = t[h];
     }
+    __threadfence();       // (the call behind reads this as constants, before it waits for this kernel's end)
 }
 
 int launch_prepare_okt(const OktGeom& g, const float* P1, const float* P2, void* prepared, cudaStream_t stream) {

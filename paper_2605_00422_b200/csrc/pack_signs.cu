@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(256) row_sums_kernel(const uint32_t* __restric
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ones += __shfl_xor_sync(0xFFFFFFFFu, ones, o);
     if (lane == 0) rowsum[row] = 2 * ones - (int32_t)(words * 32);
+    __threadfence();
 }
 
 int launch_row_sums(const uint32_t* packed, int64_t N, int64_t K, int32_t* rowsum, cudaStream_t stream) {

@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(256) prepare_rot_kernel(RotGeom g, const float
     const int tid = blockIdx.x * blockDim.x + threadIdx.x, nt = gridDim.x * blockDim.x;
     split_factor<false>(P2, g.n2, 0, rows2, g.n2p, 1.f, [&](int r, int k2) { return t2 + (size_t)r * g.s2 + 4 * k2; }, (size_t)rows2 * g.s2, tid, nt);
     split_factor<true>(P1, g.n1, 0, rows1, rows1, pow2f(e1), [&](int r, int k2) { return t1 + (size_t)r * g.s1 + 4 * k2; }, (size_t)rows1 * g.s1, tid, nt);
+    __threadfence();       // (the call behind reads this as constants, before it waits for this kernel's end)
 }
 
 int launch_prepare_rot(const RotGeom& g, const float* P1, const float* P2, void* prepared, cudaStream_t stream) {

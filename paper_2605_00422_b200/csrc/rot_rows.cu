@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(256) prepare_rows_kernel(RotRowsGeom g, const 
     __shared__ uint32_t red[8];
     const int e2 = rot_rows_split(g, P1, P2, prepared + kRotHeader, red, blockIdx.x * blockDim.x + threadIdx.x, gridDim.x * blockDim.x);
     if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int*>(prepared) = e2;
+    __threadfence();       // (the call behind reads this as constants, before it waits for this kernel's end)
 }
 int launch_prepare_rows(const RotRowsGeom& g, const float* P1, const float* P2, void* prepared, cudaStream_t stream) {
     ProfScope prof(kProfPrepare, stream);

@@ -656,3 +656,30 @@ def test_pushed_sums_on_two_streams(bwla, fmt, M):
         check_product(first, va, vw, exact=True)
         assert all(torch.equal(first, y) for y in rest)
     assert all(bwla.bwla_check_status(x) == 0 for ws in wss for x in ws)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("n1,n2", [(32, 64), (64, 80), (86, 128), (160, 160)])
+@pytest.mark.parametrize("M", [1, 300])
+def test_a_layer_is_used_at_once(bwla, fmt, n1, n2, M):
+    """Quantised weights, prepared factors and the first call one behind the other, nothing synchronised between them, in memory that held
+    another layer before."""
+    K, N = n1 * n2, 256
+    rng = np.random.default_rng([n1, n2, M, 41])
+    sets = [(dev(haar(rng, n1)), dev(haar(rng, n2)), torch.randn(N, K, device="cuda")) for _ in range(3)]
+    x = torch.randn(M, K, device="cuda").bfloat16()
+    q = bwla.bwla_fp4_quantize_rows(sets[0][2], FORMATS[fmt])
+    want = []
+    for P1, P2, W in sets:
+        layer = bwla.bwla_fp4_layer_create(P1, P2, FORMATS[fmt], *bwla.bwla_fp4_quantize_rows(W, FORMATS[fmt], *q))
+        torch.cuda.synchronize()
+        want.append(bwla.bwla_fp4_layer_linear(layer, x))
+        torch.cuda.synchronize()
+    for _ in range(4):
+        got = []
+        for P1, P2, W in sets:
+            layer = bwla.bwla_fp4_layer_create(P1, P2, FORMATS[fmt], *bwla.bwla_fp4_quantize_rows(W, FORMATS[fmt], *q))
+            got.append(bwla.bwla_fp4_layer_linear(layer, x))
+            bwla.bwla_fp4_layer_destroy(layer)
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(got, want))
