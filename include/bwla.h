@@ -284,7 +284,9 @@ int bwla_fp4_quantize_rows(const void* x, int dtype, int64_t M, int64_t K, int64
 
 /*
  * The values that codes stand for: code * block scale (exact) * row scale in fp32, rounded to `dtype` (BWLA_DTYPE_F32 or BF16).
- * What the quantiser has made comes back exactly in either type.   out device [M][ldo], ldo >= K
+ * What the quantiser has made comes back exactly in either type, but for BWLA_FP4_NV at the ends of fp32's range: values above
+ * 1760 * 2^117 in a block with one above 2016 * 2^117 come back as infinities (the block's scale is 352 * 2^117 there, and 6 times that
+ * is beyond fp32), and in bf16 what has bits below 2^-133 is rounded (rows of a scale below 2^-123).   out device [M][ldo], ldo >= K
  */
 int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const float* row_scales, int64_t M, int64_t K, int format,
                          void* out, int dtype, int64_t ldo, void* stream);
@@ -292,8 +294,8 @@ int bwla_fp4_expand_rows(const uint8_t* codes, const uint8_t* scales, const floa
 /*
  * Product of two operands of one format, M rows of activations and N rows of weights:
  *   out[m][n] = bf16( a_rows[m] * w_rows[n] * sum_k a[m][k] * w[n][k] )
- * with fp32 sums on the block-scaled tensor cores (their accumulation truncates: a sum over K is off by at most K/64 units
- * of 2^-23 of its largest partial sum).
+ * with fp32 sums on the block-scaled tensor cores, whose accumulation truncates.  Before the rounding to bf16 an output is off by at most
+ * (K/64 + 4) 2^-22 of |a_rows[m] * w_rows[n]| * sum_k |a[m][k]| |w[n][k]|, sums of parts of K and both row scales counted.
  * All inputs, the weights' codes and scales among them, may be what the preceding kernel of `stream` makes, whoever's kernel it is.
  *   out_bf16  device, bf16 [M][ldo], ldo >= N; columns beyond N are left as they are.  M == 0 or N == 0 is a no-op.
  *   workspace device, 256-byte aligned, of bwla_fp4_gemm_workspace_bytes; its first 256 bytes (status words) must be zero

@@ -235,7 +235,8 @@ int launch_fp4_quantize(const void* x, int dtype, int64_t M, int64_t K, int64_t 
 
 // ---------------------------------------------------------------------------------------------
 // values of codes: code * block scale (exact) * row scale in fp32, then to the output's type.  bf16 holds every product of a code, a
-// scale and a power of two, so what the quantiser has made comes back exactly.
+// scale and a power of two, so what the quantiser has made comes back exactly, inside the types' ranges: 6 * 352 * 2^117 is an infinity
+// (a scale that NV blocks with a value above 2016 * 2^117 have), and bf16 rounds below 2^-133 (rows of NV scaled by less than 2^-123).
 // ---------------------------------------------------------------------------------------------
 struct Fp4ExpandParams {
     const uint8_t *codes, *scales; const float* row_scales;

@@ -683,3 +683,31 @@ def test_a_layer_is_used_at_once(bwla, fmt, n1, n2, M):
             bwla.bwla_fp4_layer_destroy(layer)
         torch.cuda.synchronize()
         assert all(torch.equal(u, v) for u, v in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_expansion_at_the_ends_of_fp32(bwla, dtype):
+    """Which values come back as infinities, and what bf16 cannot hold: the header's numbers.  MX has neither."""
+    rng = np.random.default_rng(51)
+    unit = 2.0 ** 117
+    x = np.zeros((64, 64))
+    tops = np.r_[np.linspace(1700, 2047, 60), 2015.999, 2016.0, 2016.001, 2047.9]
+    x[:, :16] = tops[:, None] * rng.choice([-1, 1], (64, 16)) * np.r_[1, rng.uniform(0.8, 1, 15)]
+    x[:, 16:32] = rng.uniform(-2015, 2015, (64, 16))             # (a block of the same row without such a value)
+    x[:, 1], x[:, 2] = 1760.0, 1760.001
+    x[:, 0] = tops
+    top = np.ascontiguousarray(x * unit, np.float32)
+    small = (rng.uniform(-1, 1, (64, 64)) * np.exp2(rng.integers(-127, -112, (64, 1)))).astype(np.float32)
+    for fmt in ("nv", "mx"):
+        for rows in (top, small):
+            q = bwla.bwla_fp4_quantize_rows(dev(rows), FORMATS[fmt])
+            got = bwla.bwla_fp4_expand_rows(*q, FORMATS[fmt], dtype=dtype).double().cpu()
+            want = torch.from_numpy(fp4.expand(*fp4.quantize(rows.astype(np.float64), fmt), fmt))      # (exact: 64 bits have room)
+            beyond = want.abs() >= 2.0 ** 128
+            v = np.abs(rows.astype(np.float64)) / unit
+            says = (v > 1760) & np.repeat(v.reshape(64, 4, 16).max(2) > 2016, 16, 1) if fmt == "nv" else np.zeros(v.shape, bool)
+            assert np.array_equal(beyond.numpy(), says)
+            assert torch.equal(torch.isinf(got), beyond) and torch.equal(got[~beyond], want.to(dtype).double()[~beyond])
+            exact = got == want
+            assert exact[~beyond].all() or (fmt == "nv" and dtype is torch.bfloat16 and rows is small and exact[q[2].cpu() >= 2.0 ** -123].all())
+    assert (tops > 2016).sum() > 3
