@@ -1,4 +1,5 @@
 // extern "C" boundary of the microscaled 4-bit path: argument checks, workspace carving, dispatch.
+#include <algorithm>
 #include <cstdlib>
 
 #include "fp4.cuh"
@@ -42,16 +43,27 @@ static int check_layer_device(const bwla_fp4_layer* L) {
 }
 
 // What the rotation needs beside its outputs: status words, and room for its fp32 outputs (with 8-bit codes and scales that nobody reads) where
-// a call may go to a kernel that has no microscaled codes.
+// a call may go to a kernel that has no microscaled codes, or for some rows of x where only rows off 16 bytes would (at y).
 struct Fp4RotLayout { size_t y, scales, codes, total; };
 static Fp4RotLayout rot_layout_of(const RotGeom& g, int64_t M) {
     Fp4RotLayout w{};
     w.y = w.scales = w.codes = w.total = kStatusBytes;
     if (!rot_fp4_unfused(g)) return w;
+    if (rot_fp4_staged(g)) {
+        w.total = w.y + align_up((size_t)std::min(M, kFp4StageRows) * (size_t)g.K * 2, 256);
+        return w;
+    }
     w.scales = w.y + align_up((size_t)M * (size_t)g.K * 4, 256);
     w.codes = w.scales + align_up((size_t)M * 4, 256);
     w.total = w.codes + align_up((size_t)M * (size_t)g.K, 256);
     return w;
+}
+
+// Rows of 2-byte values from anywhere on 2 bytes to aligned ones.
+__global__ void __launch_bounds__(256) stage_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx, int K, uint32_t* __restrict__ out) {
+    const uint16_t* const from = x + (int64_t)blockIdx.x * ldx;
+    uint32_t* const to = out + (int64_t)blockIdx.x * (K >> 1);
+    for (int i = threadIdx.x; i < K >> 1; i += blockDim.x) to[i] = from[2 * i] | (uint32_t)from[2 * i + 1] << 16;
 }
 
 // chained: the outputs are scratch of the call, read by a kernel that waits for this one
@@ -63,9 +75,28 @@ static int rotate_quant(const PreparedFactors& f, const float* P1, const float* 
     pr.fp4 = format == BWLA_FP4_NV ? 2 : 1; pr.hold = !chained;
     pr.fp4_codes = codes; pr.fp4_scales = scales; pr.fp4_rows = row_scales;
     bool taken = false;
+    const Fp4RotLayout w = rot_layout_of(f.geom, M);
+    if (rot_fp4_staged(f.geom) && !rot_accepts_x(x, ldx)) {
+        // (in stream order throughout: the copies are ordinary launches, so each waits for the rotation of the rows before, and that for it)
+        const int64_t K = f.geom.K, tile_row = (int64_t)fp4_col_tiles(K, format) * 512;
+        uint8_t* const rows = (uint8_t*)(base + w.y);
+        for (int64_t m = 0; m < M; m += kFp4StageRows) {
+            const int64_t count = std::min(M - m, kFp4StageRows);
+            {
+                ProfScope prof(kProfPrepare, stream);
+                stage_rows_kernel<<<(unsigned)count, 256, 0, stream>>>((const uint16_t*)x + m * ldx, ldx, (int)K, (uint32_t*)rows);
+                const int st = after_launch();
+                if (st != BWLA_OK) return st;
+            }
+            pr.fp4_codes = codes + m * (K / 2); pr.fp4_scales = scales + m / 128 * tile_row; pr.fp4_rows = row_scales ? row_scales + m : nullptr;
+            const int st = launch_rot_fp4(f.geom, rows, count, K, pr, (uint32_t*)base, &taken, stream);
+            if (st != BWLA_OK) return st;
+            if (!taken) return BWLA_ERR_UNSUPPORTED;          // (the plans would have to disagree)
+        }
+        return BWLA_OK;
+    }
     int st = launch_rot_fp4(f.geom, x, M, ldx, pr, (uint32_t*)base, &taken, stream);
     if (st != BWLA_OK || taken) return st;
-    const Fp4RotLayout w = rot_layout_of(f.geom, M);
     if (w.codes == w.y) return BWLA_ERR_UNSUPPORTED;          // (rot_fp4_unfused and launch_rot_fp4 would have to disagree)
     RotProblem y{};
     y.prepared = f.base; y.many = f.many; y.P1 = P1; y.P2 = P2;

@@ -426,6 +426,14 @@ inline bool rot_fp4_unfused(const RotGeom& g) {
     const bool mma = rot_fp4_groups(g, &groups), many = rot_rows_geometry(g.n1, g.n2, 1, &rows) && rot_rows_fp4(rows);
     return !mma || (!many && !rot_mma_always(g));
 }
+// Of those the factors whose every call rot_rows.cu takes, but for rows off 16 bytes: these are copied to aligned ones, kFp4StageRows (whole scale
+// tiles) at a time, so that the room does not grow with the tokens (86 x 128, 4096 tokens: 23 MB, for 225 of rotated values).
+constexpr int64_t kFp4StageRows = 1024;
+inline bool rot_fp4_staged(const RotGeom& g) {
+    RotRowsGeom rows;
+    int groups = 1;
+    return !rot_fp4_groups(g, &groups) && rot_rows_geometry(g.n1, g.n2, 1, &rows) && rot_rows_fp4(rows);
+}
 // Whether rows of weights are binarised there and not by rot_mma.cu: up to 80 columns (its error is smaller then), more rows than half of the SMs, and
 // factors for which a step, whose time does not depend on n1, is the shorter one.  us of 4000 to 5120 rows, rot_mma.cu | rot_rows.cu, fp32 and bf16:
 //    64 x 64  94 |  85   64 | 51      64 x 48  76 | 75   55 | 45      48 x 48  58 | 70   42 | 43      64 x 32  49 | 66   36 | 39

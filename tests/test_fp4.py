@@ -283,3 +283,12 @@ def test_pointers_off_their_elements_are_refused(lib):
     import torch
     if not torch.cuda.is_available():          # on their elements they are taken: what is refused here is the missing device
         assert quantize(two, 1, p) == quantize(two, 2, p) == expand(two, 1, None) == gemm(None, None, two) == rotate(two, p) == create(None) == -2
+
+
+@pytest.mark.parametrize("n1,n2", [(86, 128), (108, 128), (112, 128)])
+def test_room_for_rows_off_16_bytes_is_bounded(lib, n1, n2):
+    """Factors whose every aligned call writes codes at once keep no rotated values, only some rows to copy unaligned ones to."""
+    K = n1 * n2
+    size = lambda M: lib.bwla_rotate_quant_fp4_workspace_bytes(M, K, n1, n2)
+    assert size(1) <= 256 + 2 * K + 256 and size(4096) == size(1 << 20) == 256 + 1024 * 2 * K
+    assert size(0) == 256 and all(size(M) <= size(M + 1) for M in (0, 1, 5, 127, 1023, 1024))

@@ -711,3 +711,23 @@ def test_expansion_at_the_ends_of_fp32(bwla, dtype):
             exact = got == want
             assert exact[~beyond].all() or (fmt == "nv" and dtype is torch.bfloat16 and rows is small and exact[q[2].cpu() >= 2.0 ** -123].all())
     assert (tops > 2016).sum() > 3
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("n1,n2", [(86, 128), (108, 128), (112, 128)])
+@pytest.mark.parametrize("M", [1, 130, 1024, 2500])
+def test_rows_off_16_bytes_have_the_codes_of_aligned_ones(bwla, fmt, n1, n2, M):
+    K, N = n1 * n2, 200
+    rng = np.random.default_rng([n1, M, 61])
+    P1, P2 = dev(haar(rng, n1)), dev(haar(rng, n2))
+    x = torch.randn(M, K + 3, device="cuda").bfloat16()[:, 1:K + 1]
+    layer = bwla.bwla_fp4_layer_create(P1, P2, FORMATS[fmt], *bwla.bwla_fp4_quantize_rows(torch.randn(N, K, device="cuda"), FORMATS[fmt]))
+    ws = bwla.new_fp4_layer_workspace(layer, M)
+    nb = K // fp4.BLOCK[fmt]
+    for call in (lambda x: bwla.bwla_fp4_layer_rotate_quant(layer, x, workspace=ws), lambda x: bwla.bwla_rotate_quant_fp4(x, P1, P2, FORMATS[fmt])):
+        got, want = call(x), call(x.contiguous())
+        assert torch.equal(got[0], want[0])
+        assert np.array_equal(fp4.untile(got[1].cpu().numpy(), M, nb), fp4.untile(want[1].cpu().numpy(), M, nb))
+        assert got[2] is None or torch.equal(got[2], want[2])
+    assert torch.equal(bwla.bwla_fp4_layer_linear(layer, x, workspace=ws), bwla.bwla_fp4_layer_linear(layer, x.contiguous(), workspace=ws))
+    assert bwla.bwla_check_status(ws) == 0
