@@ -14,8 +14,6 @@
 
 namespace bwla {
 
-template <bool NV>
-struct Fp4Format { static constexpr int block = NV ? 16 : 32; };
 inline int fp4_block(int format) { return format == BWLA_FP4_NV ? 16 : 32; }
 inline int64_t fp4_col_tiles(int64_t K, int format) { return (K / fp4_block(format) + 3) / 4; }      // tiles of 4 blocks along a row
 
@@ -38,12 +36,6 @@ __device__ __forceinline__ uint32_t fp4_codes8(const float (&v)[8]) {
         "mov.b32 %0, {a, b, c, d};\n\t}"
         : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return r;
-}
-// Two values, the first in the low half of a byte.
-__device__ __forceinline__ uint32_t fp4_codes2(float lo, float hi) {
-    uint32_t r;
-    asm("{\n\t.reg .b8 a;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tmov.b32 %0, {a, a, a, a};\n\t}" : "=r"(r) : "f"(lo), "f"(hi));
-    return r & 0xFFu;
 }
 // ... and back (exact)
 __device__ __forceinline__ void fp4_values8(uint32_t codes, float (&v)[8]) {
