@@ -731,3 +731,66 @@ def test_rows_off_16_bytes_have_the_codes_of_aligned_ones(bwla, fmt, n1, n2, M):
         assert got[2] is None or torch.equal(got[2], want[2])
     assert torch.equal(bwla.bwla_fp4_layer_linear(layer, x, workspace=ws), bwla.bwla_fp4_layer_linear(layer, x.contiguous(), workspace=ws))
     assert bwla.bwla_check_status(ws) == 0
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("n1,n2,M", [(32, 64, 5000), (64, 64, 4096), (64, 80, 4100), (64, 88, 2300), (86, 128, 2500), (112, 128, 1801)])
+def test_rotation_of_many_steps(bwla, fmt, n1, n2, M):
+    """Many steps a CTA follow one another: rows from all of them, the last ones among them."""
+    K = n1 * n2
+    rng = np.random.default_rng([n1, n2, M, 71])
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.randn(M, K, device="cuda", generator=g).bfloat16()
+    x[M // 2] = 0
+    P1, P2 = haar(rng, n1), haar(rng, n2)
+    at = np.unique(np.r_[rng.integers(0, M, 160), 0, M // 2, np.arange(M - 24, M)])
+    nb = K // fp4.BLOCK[fmt]
+    layer = bwla.bwla_fp4_layer_create(dev(P1), dev(P2), FORMATS[fmt], *bwla.bwla_fp4_quantize_rows(torch.randn(8, K, device="cuda", generator=g), FORMATS[fmt]))
+    first = None
+    for codes, scales, rows in (bwla.bwla_rotate_quant_fp4(x, dev(P1), dev(P2), FORMATS[fmt]), bwla.bwla_fp4_layer_rotate_quant(layer, x), bwla.bwla_fp4_layer_rotate_quant(layer, x)):
+        byte = fp4.untile(scales.cpu().numpy(), M, nb)
+        i = torch.from_numpy(at).cuda()
+        check_rotated(bwla, x[i], P1, P2, fmt, (codes[i], dev(fp4.tile(byte[at])), None if rows is None else rows[i]))
+        again, first = first, (codes, byte)
+    assert torch.equal(again[0], first[0]) and np.array_equal(again[1], first[1]), "a call must repeat itself bit for bit"
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K", [(2500, 18944, 512), (4096, 25600, 288), (3333, 8195, 1056)])
+def test_product_of_many_full_rounds(bwla, fmt, M, N, K):
+    rng = np.random.default_rng([M, N, K, 81])
+    a, sa, va = operand(rng, M, K, fmt, integers=True)
+    w, sw, vw = operand(rng, N, K, fmt, integers=True)
+    ws = bwla.new_fp4_workspace(M, K, N)
+    out = bwla.bwla_fp4_gemm_codes(a, sa, None, w, sw, None, FORMATS[fmt], workspace=ws)
+    assert bwla.bwla_check_status(ws) == 0
+    check_product(out, va, vw, exact=True)
+
+
+def test_threads_with_layers_of_their_own(bwla):
+    """Two threads, each with a layer, a workspace and a stream."""
+    import threading
+    K, N = 64 * 64, 1024
+    jobs = []
+    for i, (fmt, M) in enumerate((("mx", 3), ("nv", 300))):
+        rng = np.random.default_rng([i, 91])
+        w = bwla.bwla_fp4_quantize_rows(torch.randn(N, K, device="cuda"), FORMATS[fmt])
+        layer = bwla.bwla_fp4_layer_create(dev(haar(rng, 64)), dev(haar(rng, 64)), FORMATS[fmt], *w)
+        xs = [torch.randn(M, K, device="cuda").bfloat16() for _ in range(3)]
+        jobs.append((layer, bwla.new_fp4_layer_workspace(layer, M), torch.cuda.Stream(), xs, [bwla.bwla_fp4_layer_linear(layer, x) for x in xs], []))
+    torch.cuda.synchronize()
+
+    def work(layer, ws, stream, xs, want, bad):
+        with torch.cuda.stream(stream):
+            for _ in range(40):
+                got = [bwla.bwla_fp4_layer_linear(layer, x, workspace=ws) for x in xs]
+                stream.synchronize()
+                bad.extend(1 for u, v in zip(got, want) if not torch.equal(u, v))
+        bad.append(0)
+
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert all(j[5] == [0] for j in jobs) and all(bwla.bwla_check_status(j[1]) == 0 for j in jobs)
