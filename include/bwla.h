@@ -310,7 +310,10 @@ int bwla_fp4_gemm_codes(const uint8_t* a_codes, const uint8_t* a_scales, const f
  * Online OKT (Sec. 3.1) and the quantiser above: codes and scales of Y_t = P1^T * reshape(x_t, n1 x n2) * P2, for activations and, with
  * rows of a weight matrix as x, for the weights that meet them.  Y has the accuracy of bwla_rotate_quant_act's (1e-6 of a token's
  * full scale); a code or block scale can differ from the exact Y's only where that decides.
- *   x_bf16 device, bf16 [M][ldx]; P1, P2 as for bwla_rotate_quant_act.  Factor sizes the tensor-core rotation does not take
+ * A call repeats itself bit for bit; the same token in a batch of another size may go to another kernel, and a code or scale that
+ * such an error decides may then be the next one.
+ *   x_bf16 device, bf16 [M][ldx]; P1, P2 as for bwla_rotate_quant_act, constants as those of bwla_w1ax_linear are: they are read
+ *   while the preceding kernel of `stream` may still run, so they must not be what it makes.  Factor sizes the tensor-core rotation does not take
  *   (n2 % 8 != 0, n2 > 256, n1 > 192) return BWLA_ERR_UNSUPPORTED.
  *   workspace of bwla_rotate_quant_fp4_workspace_bytes (0 for factor sizes that are not taken), its first 256 bytes as above
  */

@@ -12,7 +12,7 @@
 //   all      epilogue: token t of the tile is finished by CTA t mod S of the cluster.  The sums lie where the stages were, [token][row], and the owners
 //            read them between two cluster barriers.  Up to four tokens every CTA pushes its sums to the owners instead, who have room
 //            beside their stages, and a barrier of the owner's counts them: nobody else waits for sums (one token 4096 x 4096 4.2 -> 3.9 us, 5120 x 5120
-//            NV 5.7 -> 5.3; but 32 tokens of 5120 x 5120 6.2 -> 7.0: words, where reading takes 16 bytes).  Rows of 256 bytes are stored.
+//            NV 5.7 -> 5.3, with weights asked for ahead; but 32 tokens of 5120 x 5120 6.2 -> 7.0: words, where reading takes 16 bytes).  Rows of 256 bytes are stored.
 #include "fp4.cuh"
 #include "tensor_map.cuh"
 #include "umma_wait.cuh"

@@ -243,9 +243,9 @@ inline bool rot_fp4_groups(const RotGeom& g, int* groups) {
 constexpr int kFp4Sms = 148, kFp4Pairs = 74;             // what the plans count with; a device that holds fewer takes more rounds
 constexpr int kFp4MaxSplit = 8;
 constexpr size_t kFp4PartBytes = 2 * 128 * 256 * 4;      // the sums of a tile of a pair
-// How many CTAs K is cut over.  One an SM leaves room for the kernel behind this one to start beside it (its weights are on their way when
-// this one ends); more pay where each still has four k-blocks of 256, and up to 13 for 8 SMs clusters of any size fit at once.  In a chain of
-// calls, us, parts 1 | 2 | 3 | 4 | 5 | 6 | 7 | 8:  5120 x 5120, 1 token 6.6 5.4 5.3 5.1 5.1 5.2 9.1 8.5;  4096 x 4096 5.3 4.5 4.5 4.2 4.5 4.5 5.0 4.9;
+// How many CTAs K is cut over.  One an SM leaves room for the kernel behind this one to start beside it (a layer's weights are on their way, others
+// in the L2, when this one ends); more pay where each still has four k-blocks of 256, and up to 13 for 8 SMs clusters of any size fit at once.  In a
+// chain of calls with weights asked for ahead, us, parts 1 | 2 | 3 | 4 | 5 | 6 | 7 | 8:  5120 x 5120, 1 token 6.6 5.4 5.3 5.1 5.1 5.2 9.1 8.5;  4096 x 4096 5.3 4.5 4.5 4.2 4.5 4.5 5.0 4.9;
 // 25600 -> 5120, 64 tokens 33 21 17.3 16.1 15.4 15.1 23.4 22.1;  4096 -> 11008, 16 tokens 6.9 6.5 7.0 10.7 ...;  25600 -> 1024, 1 token 23 13.4 10.2
 // 8.3 7.6 6.8 6.8 6.4.
 inline int fp4_split_parts(int64_t M, int64_t K, int64_t N, int tok) {
@@ -283,6 +283,9 @@ inline Fp4SplitPlan fp4_split_plan(int64_t M, int64_t K, int64_t N, bool nv) {
 }
 // Pairs, whole tiles of each, and whether the rest is cut by k: the last full round with what does not fill a round, or tiles in two where there
 // are no more than half as many as pairs.  A cut costs some 10 us (the sums of parts go through the L2), so it has to save more: time in ns.
+// A k-block is counted with 360 ns (what it takes when the power limit is reached, 300 in short bursts), DRAM and the outputs with nothing, so that the
+// estimate is far too short where these bound the call: 4096 tokens, K 256 -> 18944 (155 MB of outputs) 11.8 us, takes 54 (MX) and 65 (NV); 200 tokens
+// 11008 -> 25600 36.9, takes 40 and 42.  These calls go to the pairs either way.
 struct Fp4PairPlan { int pairs, whole; bool cut; int64_t ns; };
 inline Fp4PairPlan fp4_pair_plan(int64_t M, int64_t K, int64_t N, int device_pairs, bool may_cut) {
     const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), kblocks = (K + 255) / 256, most = std::min(device_pairs, kFp4Pairs);
@@ -297,9 +300,10 @@ inline Fp4PairPlan fp4_pair_plan(int64_t M, int64_t K, int64_t N, int device_pai
     return r;
 }
 inline size_t fp4_part_bytes(const Fp4PairPlan& r) { return r.cut ? (size_t)r.pairs * 2 * kFp4PartBytes : 0; }
-// Which of the two takes a product.  us, fp4_split.cu | fp4_pair.cu (MX; * cut): 257 x 4096 x 4096 (tokens x K x N) 6.8 | 12; 333 x 11008 x 4096 14.2 | 24.5;
+// Which of the two takes a product (by the sizes of MX for both formats: NV has a sixteenth more bytes in either).  us in short bursts, one call behind
+// another, fp4_split.cu | fp4_pair.cu (MX; * cut): 257 x 4096 x 4096 (tokens x K x N) 6.8 | 12; 333 x 11008 x 4096 14.2 | 24.5;
 // 512 x 4096 x 4096 7.8 | 11.8; 200 x 25600 x 5120 23.7 | 34 *; 512 x 5120 x 25600 45 | 35; 1024 x 25600 x 5120 104 | 55 *; 2048 x 5120 x 8192 56 | 34; 4096 x 5120 x
-// 25600 318 | 194 (without a flush of the L2 between calls).
+// 25600 318 | 194.  (With calls for seconds the power limit takes the clock to 1.4 and 1.3 GHz: the pairs' 55 and 194 become 64 and 218.)
 inline bool fp4_in_pairs(int64_t M, int64_t K, int64_t N) {
     if (M <= 128 || N <= 0) return false;                // (without weight rows there is no tile to plan for)
     if ((M + 127) / 128 > 65535) return true;            // (the same of tiles of 128)

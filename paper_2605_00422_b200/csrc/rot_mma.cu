@@ -1128,6 +1128,10 @@ int launch_rot_fp4(const RotGeom& base, const void* x, int64_t M, int64_t ldx, c
     // (as launch_rot has it for codes: many tokens on rot_rows.cu where it can and is the faster one)
     RotRowsGeom rows;
     const bool can = vec && rot_rows_supports(base, 1, &problem) && rot_rows_geometry(base.n1, base.n2, 1, &rows) && rot_rows_fp4(rows);
+    // Of few tokens rot_rows.cu takes those of more than 80 columns.  us of a layer's call with 4096 outputs in a graph, rot_rows.cu | clusters of this
+    // kernel, 1, 16 and 64 tokens (where it has room at all):  64 x 96 MX 10.2 | 10.6, 11.7 | 11.8, 12.7 | 14.0;  64 x 128 MX 11.7 | 12.6, 13.3 | 13.8,
+    // 14.6 | 17.1;  108 x 128 MX 12.8 | 15.6, 13.6 | 18.3;  108 x 128 NV 15.1 | 15.1, 15.3 | 18.9;  86 x 128 one kernel only (1 token MX 12.1, NV 14.1).
+    // NV of 64 x 96 and 64 x 128 loses a tenth by it up to some 50 tokens: 12.5 | 10.9, 13.3 | 12.2, 14.8 | 14.7 and 13.3 | 12.6, 15.1 | 13.3, 16.6 | 17.7.
     const bool faster = few ? !rot_mma_always(base) : rot_rows_faster(base, false, !problem.prepared, false, false, M, sm_count());
     if (can && (!mma || faster)) {
         const OktLowrank none{};
