@@ -75,11 +75,10 @@ static int rotate_quant(const PreparedFactors& f, const float* P1, const float* 
     pr.fp4 = format == BWLA_FP4_NV ? 2 : 1; pr.hold = !chained;
     pr.fp4_codes = codes; pr.fp4_scales = scales; pr.fp4_rows = row_scales;
     bool taken = false;
-    const Fp4RotLayout w = rot_layout_of(f.geom, M);
-    if (rot_fp4_staged(f.geom) && !rot_accepts_x(x, ldx)) {
+    if (!rot_accepts_x(x, ldx) && rot_fp4_staged(f.geom)) {
         // (in stream order throughout: the copies are ordinary launches, so each waits for the rotation of the rows before, and that for it)
         const int64_t K = f.geom.K, tile_row = (int64_t)fp4_col_tiles(K, format) * 512;
-        uint8_t* const rows = (uint8_t*)(base + w.y);
+        uint8_t* const rows = (uint8_t*)(base + rot_layout_of(f.geom, M).y);
         for (int64_t m = 0; m < M; m += kFp4StageRows) {
             const int64_t count = std::min(M - m, kFp4StageRows);
             {
@@ -97,6 +96,7 @@ static int rotate_quant(const PreparedFactors& f, const float* P1, const float* 
     }
     int st = launch_rot_fp4(f.geom, x, M, ldx, pr, (uint32_t*)base, &taken, stream);
     if (st != BWLA_OK || taken) return st;
+    const Fp4RotLayout w = rot_layout_of(f.geom, M);
     if (w.codes == w.y) return BWLA_ERR_UNSUPPORTED;          // (rot_fp4_unfused and launch_rot_fp4 would have to disagree)
     RotProblem y{};
     y.prepared = f.base; y.many = f.many; y.P1 = P1; y.P2 = P2;

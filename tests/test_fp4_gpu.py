@@ -794,3 +794,29 @@ def test_threads_with_layers_of_their_own(bwla):
     for t in threads:
         t.join()
     assert all(j[5] == [0] for j in jobs) and all(bwla.bwla_check_status(j[1]) == 0 for j in jobs)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("n1,n2,M", [(64, 64, 9), (86, 128, 9), (86, 128, 1100), (64, 88, 40)])
+def test_rows_off_16_bytes_in_a_graph(bwla, fmt, n1, n2, M):
+    K, N = n1 * n2, 320
+    rng = np.random.default_rng([n1, n2, M, 101])
+    layer = bwla.bwla_fp4_layer_create(dev(haar(rng, n1)), dev(haar(rng, n2)), FORMATS[fmt], *bwla.bwla_fp4_quantize_rows(torch.randn(N, K, device="cuda"), FORMATS[fmt]))
+    x = torch.randn(M, K + 5, device="cuda").bfloat16()[:, 3:K + 3]
+    ws, out = bwla.new_fp4_layer_workspace(layer, M), torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        bwla.bwla_fp4_layer_linear(layer, x, out=out, workspace=ws)
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            for _ in range(3):
+                bwla.bwla_fp4_layer_linear(layer, x, out=out, workspace=ws)
+        for _ in range(3):
+            x.copy_(torch.randn(M, K, device="cuda").bfloat16())
+            g.replay()
+            got = out.clone()
+            assert torch.equal(got, bwla.bwla_fp4_layer_linear(layer, x))
+    side.synchronize()
+    assert bwla.bwla_check_status(ws) == 0
